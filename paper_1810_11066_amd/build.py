@@ -1,4 +1,5 @@
-"""Build libbitserial.so in-tree with hipcc for gfx950.
+"""Build libbitserial.so (and the libraries beside it: libint8mfma.so and
+libbscache.so) in-tree with hipcc for gfx950.
 
     python -m paper_1810_11066_amd.build
 
@@ -31,6 +32,8 @@ LIB = os.path.join(HERE, "libbitserial.so")
 # the int8 matrix-core comparison baseline: a library of its own
 INT8_LIB = os.path.join(HERE, "libint8mfma.so")
 INT8_SOURCE = "int8_mfma.hip"
+# the quantized key-value cache and its attention: a library of its own
+CACHE_LIB = os.path.join(HERE, "libbscache.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # (source, object name, defines)
@@ -53,6 +56,13 @@ UNITS = ([("api.hip", "api", ()), ("quant_pack.hip", "quant_pack", ()),
 SOURCES = sorted({u[0] for u in UNITS} |
                  {"bs_internal.h", "conv_fast.h", "conv_pix.h",
                   "conv_tiled.h", "dense_rows.h"})
+
+# the cache library's units: the attention kernels are compiled once per
+# padded channel count
+CACHE_UNITS = ([("cache.hip", "cache", ()),
+                ("cache_attend.hip", "cache_attend", ())] +
+               [("cache_attend_inst.hip", "cache_attend_%d" % dp,
+                 ("BS_DP=%d" % dp,)) for dp in (64, 128, 256)])
 
 CFLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -92,23 +102,33 @@ def build_int8(verbose: bool = False, out: str = INT8_LIB) -> str:
     return out
 
 
-def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
-    """Compile and link the library (to `out`, with extra -D `defines`);
-    returns its path."""
-    extra = ["-D" + d for d in defines]
+def _build_units(units, out: str, extra, verbose: bool) -> str:
+    """Compile the units side by side and link them to `out`."""
     with tempfile.TemporaryDirectory(prefix="bs_build_") as tmp:
-        objs = [os.path.join(tmp, u[1] + ".o") for u in UNITS]
-        with cf.ThreadPoolExecutor(max_workers=min(8, len(UNITS))) as ex:
+        objs = [os.path.join(tmp, u[1] + ".o") for u in units]
+        with cf.ThreadPoolExecutor(max_workers=min(8, len(units))) as ex:
             list(ex.map(lambda a: _compile(
-                a[0][0], a[1], extra + ["-D" + d for d in a[0][2]]),
-                zip(UNITS, objs)))
+                a[0][0], a[1], list(extra) + ["-D" + d for d in a[0][2]]),
+                zip(units, objs)))
         _link(objs, out)
     if verbose:
         print("built", out)
     return out
 
 
+def build_cache(verbose: bool = False, out: str = CACHE_LIB) -> str:
+    """Compile and link the key-value cache library; returns its path."""
+    return _build_units(CACHE_UNITS, out, (), verbose)
+
+
+def build(verbose: bool = False, out: str = LIB, defines=()) -> str:
+    """Compile and link the library (to `out`, with extra -D `defines`);
+    returns its path."""
+    return _build_units(UNITS, out, ["-D" + d for d in defines], verbose)
+
+
 if __name__ == "__main__":
     build(verbose=True)
     build_int8(verbose=True)
+    build_cache(verbose=True)
     sys.exit(0)

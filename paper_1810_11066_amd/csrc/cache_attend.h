@@ -1,0 +1,705 @@
+// Attention of one new token over the pages of a quantized cache.
+//
+// A workgroup takes units of 128 tokens of one (sequence, key-value head, tile
+// of up to 16 query heads); its four waves take 32 tokens of a unit each and
+// never wait for one another until the segment ends.  Per wave and unit:
+//
+//   logits  S[token][head] = K q as v_mfma_f32_16x16x32_f16 with the codes as
+//           the A operand (row = token, k = channel) and the queries as B
+//           (column = head), 16 tokens at a time.  Lane l gets the logits of
+//           head l % 16 for the tokens 4 (l / 16) .. + 3 of each 16.
+//   softmax the running maximum and sum of a head live in its 4 lanes.
+//   values  O[channel][head] += V^T w, the same instruction: A = codes (row =
+//           channel, k = token), B = weights (column = head, k = token).  The
+//           order of k is free as long as A and B agree, so the weights stay
+//           in the lanes that computed them: k 0..7 of lane group g are the
+//           tokens 4 g .. + 3 of both halves, and lane l loads those tokens'
+//           codes.  No weight ever moves between lanes.
+//
+// Codes become float16 without conversions: 0x6400 | c is 1024 + c, and one
+// packed subtraction of 1024 + centre (128 or 8) gives the centred code c',
+// exactly.  4-bit codes in the second nibble of a byte stay there (1024 + 16
+// c): their products carry a factor of 16, which the queries (keys) or the
+// final outputs (values) of those channels take back.  With the centre in the
+// offset, value = s c' + (z + centre s), so
+//   logit = scale (s (q . c') + (z + centre s) sum q)
+//   out   = (sum_t w_t c'_t + sum_t p_t (z_t + centre s_t)) / sum_t p_t
+// with w = p s.
+//
+// Roundings: q is scaled by a power of two to below 2^10 and rounded to
+// float16: bfloat16 and float16 values keep all their bits, but for what lies
+// below 2^-30 of the row's largest; float32 queries take a second float16 for the
+// rest (22 bits together), a second MFMA into the same accumulator.  w is
+// rounded to float16 (2^-12 relative, within the 2^-12 and 2^-9 of the output
+// types; float32 calls take a second float16 too).  w = 2^7 (p / 2^m) (s / S)
+// with m the running maximum and S a power of two above every s, and 2^-10 |z|,
+// so far (z far beyond s is a row of nearly equal values, whose sums p z would
+// leave binary32); m may lag by 2^8, so w stays below 2^15 and keeps its full
+// precision down to 2^-21 of the largest weight.  Everything else is float32.
+//
+// Sharing: the units of all (sequence, head tile) pairs are numbered in one
+// row, and workgroup i of n takes units [i U / n, (i + 1) U / n): every
+// workgroup has the same work whatever the lengths.  U depends on the lengths,
+// which only the device knows; each workgroup computes it from them.  A
+// workgroup whose range covers a pair whole writes its output; otherwise it
+// leaves a partial result -- at most two, at the ends of its range -- which
+// join_kernel adds in the order of the workgroups.
+#pragma once
+
+#include "cache_internal.h"
+
+namespace bscache {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr float kNone = -3.0e38f;       // maximum of no logits
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// ---- the row of units ------------------------------------------------------
+
+// Visible tokens of a sequence: [first, length), first taken down to a
+// multiple of 16 for its tiles.
+struct Span {
+    int32_t length, first;
+    __device__ __forceinline__ int32_t start() const { return first & ~15; }
+    // a sequence without tokens has one unit: somebody writes its zeros
+    __device__ __forceinline__ int32_t units() const {
+        const int32_t n = (length - start() + kUnit - 1) / kUnit;
+        return n > 1 ? n : 1;
+    }
+};
+__device__ __forceinline__ Span span_of(const Attend& a, int32_t length) {
+    Span s;
+    s.length = length < 0 ? 0 : length < a.max_len ? length : a.max_len;
+    s.first = a.window > 0 && s.length > a.window ? s.length - a.window : 0;
+    return s;
+}
+
+// Inclusive sum over the lanes of a wave up to this one.
+__device__ __forceinline__ int32_t wave_scan(int32_t v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int32_t up = __shfl_up(v, d);
+        v += lane >= d ? up : 0;
+    }
+    return v;
+}
+
+__device__ __forceinline__ int32_t units_of(const Attend& a, int32_t b) {
+    return b < a.batch ? span_of(a, a.lengths[b]).units() : 0;
+}
+
+// Units of all sequences for one head tile.
+__device__ __forceinline__ int32_t all_units(const Attend& a, int lane) {
+    int32_t total = 0;
+    for (int32_t b = 0; b < a.batch; b += 64)
+        total += __builtin_amdgcn_readlane(wave_scan(units_of(a, b + lane), lane),
+                                           63);
+    return total;
+}
+
+// The workgroups that share u units: every one of them has at least one.
+__device__ __forceinline__ int32_t sharing(const Attend& a, int32_t u) {
+    return u < a.blocks ? u : a.blocks;
+}
+__device__ __forceinline__ int32_t range_start(int32_t i, int32_t u, int32_t n) {
+    return (int32_t)((int64_t)u * i / n);
+}
+// The workgroup whose range holds unit x.
+__device__ __forceinline__ int32_t range_of(int32_t x, int32_t u, int32_t n) {
+    return (int32_t)((((int64_t)x + 1) * n - 1) / u);
+}
+
+// Partial results: slot 2 i of workgroup i for the pair that began before its
+// range, 2 i + 1 for the pair that goes on behind it.  A slot holds [16][dim]
+// sums and [16][2] maximum (of mo, see below) and sum of weights.
+__device__ __forceinline__ float* part_of(const Attend& a, int32_t slot) {
+    return a.parts + (int64_t)slot * 16 * (a.c.dim + 2);
+}
+
+// ---- codes to float16 ------------------------------------------------------
+
+__device__ __forceinline__ uint32_t minus(uint32_t pair, _Float16 bias) {
+    const half2v b = {bias, bias};
+    return __builtin_bit_cast(uint32_t,
+                              __builtin_bit_cast(half2v, pair) - b);
+}
+
+// Channel-major operand of the keys: 8 codes of one token as 4 words of two
+// float16 each.  8 bits: x, y hold 4 codes each, in order.  4 bits: x holds 8
+// codes; the pairs are (0,4) (1,5) (2,6) (3,7), the second and fourth times 16.
+template <int BITS>
+__device__ __forceinline__ half8v key_operand(uint32_t x, uint32_t y) {
+    u32x4 f;
+    if constexpr (BITS == 8) {
+        f[0] = __builtin_amdgcn_perm(0x64646464u, x, 0x04010400u);
+        f[1] = __builtin_amdgcn_perm(0x64646464u, x, 0x04030402u);
+        f[2] = __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u);
+        f[3] = __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = minus(f[i], (_Float16)1152.0f);
+    } else {
+        const uint32_t h = x >> 8;
+        f[0] = minus((x & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f);
+        f[1] = minus((x & 0x00F000F0u) | 0x64006400u, (_Float16)1152.0f);
+        f[2] = minus((h & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f);
+        f[3] = minus((h & 0x00F000F0u) | 0x64006400u, (_Float16)1152.0f);
+    }
+    return __builtin_bit_cast(half8v, f);
+}
+// Channel of element e (0..7) of that operand, and its factor.
+template <int BITS>
+__device__ __forceinline__ constexpr int key_channel(int e) {
+    return BITS == 8 ? e : (e >> 1) + 4 * (e & 1);
+}
+template <int BITS>
+__device__ __forceinline__ constexpr float key_factor(int e) {
+    return BITS == 4 && ((e >> 1) & 1) ? 1.0f / 16.0f : 1.0f;
+}
+
+// Token-major operands of the values: from 4 codes of each of 8 tokens (8
+// bits: a word each; 4 bits: the low half of a word each) one operand for each
+// of the 4 channels; of 4-bit codes channels 1 and 3 are times 16.
+template <int BITS>
+__device__ __forceinline__ void value_operands(const uint32_t (&x)[8],
+                                               half8v (&f)[4]) {
+    u32x4 r[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const uint32_t a = x[2 * p], b = x[2 * p + 1];
+        if constexpr (BITS == 8) {
+            const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x05010400u);
+            const uint32_t hi = __builtin_amdgcn_perm(b, a, 0x07030602u);
+            r[0][p] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u);
+            r[1][p] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u);
+            r[2][p] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u);
+            r[3][p] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                r[i][p] = minus(r[i][p], (_Float16)1152.0f);
+        } else {
+            const uint32_t v = __builtin_amdgcn_perm(b, a, 0x05040100u);
+            const uint32_t h = v >> 8;
+            r[0][p] = minus((v & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f);
+            r[1][p] = minus((v & 0x00F000F0u) | 0x64006400u, (_Float16)1152.0f);
+            r[2][p] = minus((h & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f);
+            r[3][p] = minus((h & 0x00F000F0u) | 0x64006400u, (_Float16)1152.0f);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __builtin_bit_cast(half8v, r[i]);
+}
+template <int BITS>
+__device__ __forceinline__ constexpr float value_factor(int channel) {
+    return BITS == 4 && (channel & 1) ? 1.0f / 16.0f : 1.0f;
+}
+
+__device__ __forceinline__ f32x4 mfma(half8v a, half8v b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Over the 4 lanes of a head.
+template <class F>
+__device__ __forceinline__ float over_groups(float v, F f) {
+    v = f(v, __shfl_xor(v, 16));
+    return f(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+
+template <bool TWO>
+__device__ __forceinline__ void load_q(const void* q, int64_t at, int dtype,
+                                       float (&x)[8]) {
+    if constexpr (TWO) load8<kF32>(q, at, x);
+    else if (dtype == kF16) load8<kF16>(q, at, x);
+    else load8<kBF16>(q, at, x);
+}
+__device__ __forceinline__ void store_out(void* out, int64_t at, int dtype,
+                                          f32x4 v) {
+    if (dtype == kF32) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = v;
+    } else {
+        const u32x2 w = dtype == kF16
+            ? u32x2{pack2<kF16>(v[0], v[1]), pack2<kF16>(v[2], v[3])}
+            : u32x2{pack2<kBF16>(v[0], v[1]), pack2<kBF16>(v[2], v[3])};
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) = w;
+    }
+}
+
+// ---- the kernel ------------------------------------------------------------
+
+// The codes of a wave's 32 tokens as they are loaded.  Keys: lane l has, of
+// token l % 16 of each half, the 16-code chunks l / 16 + 4 j.  Values: of the
+// 8 tokens of its lane group, the DP / 16 codes from DP / 16 (l % 16) on.
+template <int DP, int KB, int VB>
+struct Codes {
+    static constexpr int kChunks = DP / 64;        // 16-code chunks a lane
+    static constexpr int kKeyWords = KB / 2;       // words of a chunk: 4 or 2
+    static constexpr int kOwn = DP / 16;           // value channels a lane
+    static constexpr int kValueWords = kOwn * VB >= 32 ? kOwn * VB / 32 : 1;
+    uint32_t k[2][kChunks][kKeyWords];
+    uint32_t v[8][kValueWords];
+};
+
+// N words from a 4 N-byte aligned address (2 bytes where HALF).
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p,
+                                           uint32_t (&w)[N]) {
+    if constexpr (N == 1) {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (N == 2) {
+        const u32x2 t = *reinterpret_cast<const u32x2*>(p);
+        w[0] = t[0], w[1] = t[1];
+    } else {
+        static_assert(N == 4);
+        const u32x4 t = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = t[i];
+    }
+}
+
+// Where the two halves of a wave's tile lie: the row of each half's first
+// token, and whether its page is one of the cache.  Half a tile never leaves
+// a page (pages are multiples of 16 tokens).
+struct Tile {
+    int32_t token;          // first token
+    int64_t row[2];
+    bool there[2];
+};
+
+template <int DP, int KB, int VB, bool TWO>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
+    const Attend a) {
+    using C = Codes<DP, KB, VB>;
+    constexpr int kSteps = DP / 32;             // MFMAs of the logits
+    constexpr int kOwn = C::kOwn;
+    constexpr float kCentreK = KB == 8 ? 128.0f : 8.0f;
+    constexpr float kCentreV = VB == 8 ? 128.0f : 8.0f;
+    __shared__ float sm_o[kWaves][16][DP + 4];
+    __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = lane & 15, group = lane >> 4;
+    const int dim = a.c.dim;
+    const int32_t pairs = a.c.kv_heads * a.head_tiles;
+
+    // this workgroup's units and the sequence of the first
+    const int32_t total = all_units(a, lane) * pairs;
+    const int32_t sharers = sharing(a, total);
+    const int32_t self = blockIdx.x;
+    if (self >= sharers) return;
+    int32_t unit = range_start(self, total, sharers);
+    const int32_t unit_end = range_start(self + 1, total, sharers);
+    int32_t seq = 0, before = 0;     // units before seq, in one head tile
+    for (int32_t b = 0;; b += 64) {
+        const int32_t own = units_of(a, b + lane);
+        const int32_t sum = wave_scan(own, lane);
+        const int32_t all = __builtin_amdgcn_readlane(sum, 63);
+        // (units of 64 sequences times pairs stay within total)
+        if (unit < (before + all) * pairs) {
+            const uint64_t past = __ballot((before + sum) * pairs > unit);
+            const int at = __builtin_ctzll(past);
+            seq = b + at;
+            before += __builtin_amdgcn_readlane(sum - own, at);
+            break;
+        }
+        before += all;
+    }
+    seq = __builtin_amdgcn_readfirstlane(seq);
+
+    // lane offsets, in bytes, of the codes within 16 rows; lanes behind the
+    // last channel read their row's first codes (their products are dropped)
+    const int k_row = dim * KB / 8, v_row = dim * VB / 8;
+    uint32_t k_at[C::kChunks];
+#pragma unroll
+    for (int j = 0; j < C::kChunks; ++j) {
+        const int chunk = group + 4 * j;
+        k_at[j] = head * k_row + (chunk * 16 < dim ? chunk * 2 * KB : 0);
+    }
+    const uint32_t v_at =
+        4 * group * v_row + (head * kOwn < dim ? head * kOwn * VB / 8 : 0);
+
+    while (unit < unit_end) {
+        const Span span = span_of(a, a.lengths[seq]);
+        const int32_t units = span.units();
+        const int32_t rel = unit - before * pairs;
+        const int32_t pair = rel / units;
+        const int32_t c0 = rel - pair * units;
+        const int32_t c1 =
+            units - c0 < unit_end - unit ? units : c0 + unit_end - unit;
+        const int32_t kvh = pair / a.head_tiles;
+        const int32_t tile16 = pair - kvh * a.head_tiles;
+        const int32_t h0 = kvh * a.group + tile16 * 16;
+        const int32_t heads =
+            a.group - tile16 * 16 < 16 ? a.group - tile16 * 16 : 16;
+
+        // ---- tiles and their loads
+        C codes;
+        u32x4 ks[2], vs[2];
+        const int32_t* table = a.table + (int64_t)seq * a.max_pages;
+        auto find = [&](int32_t c) {
+            Tile t;
+            t.token = span.start() + c * kUnit + wave * 32;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int32_t at = t.token + 16 * s;
+                const bool in = at < span.length && c < c1;
+                const uint32_t p = in ? a.c.by_page.div(at) : 0;
+                const uint32_t page = table[p];
+                t.there[s] = in && page < a.c.pages;
+                t.row[s] = t.there[s]
+                    ? row_of(a.c, page, kvh, at - p * a.c.by_page.d)
+                    : row_of(a.c, 0, kvh, 0);
+            }
+            return t;
+        };
+        auto load_keys = [&](const Tile& t) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint8_t* base = a.c.codes[0] + t.row[s] * k_row;
+#pragma unroll
+                for (int j = 0; j < C::kChunks; ++j)
+                    load_words(base + k_at[j], codes.k[s][j]);
+            }
+        };
+        auto load_steps = [&](const Tile& t) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                ks[s] = *reinterpret_cast<const u32x4*>(
+                    a.c.steps[0] + t.row[s] + 4 * group);
+                vs[s] = *reinterpret_cast<const u32x4*>(
+                    a.c.steps[1] + t.row[s] + 4 * group);
+            }
+        };
+        auto load_values = [&](const Tile& t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint8_t* p = a.c.codes[1] + t.row[i >> 2] * v_row + v_at +
+                                   (i & 3) * v_row;
+                if constexpr (kOwn * VB < 32)
+                    codes.v[i][0] = *reinterpret_cast<const uint16_t*>(p);
+                else
+                    load_words(p, codes.v[i]);
+            }
+        };
+        Tile now = find(c0);
+        load_keys(now);
+        load_steps(now);
+        load_values(now);
+        Tile next = find(c0 + 1);
+
+        // ---- the queries of this lane's head as B operands
+        half8v q_hi[kSteps], q_lo[TWO ? kSteps : 1];
+        float q_scale, q_sum;       // of logits in units of log2
+        {
+            float x[kSteps][8], top = 0.0f, sum = 0.0f;
+            const int64_t base = seq * a.q_stride +
+                                 (int64_t)(h0 + (head < heads ? head : 0)) * dim;
+            const bool mine = head < heads;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int chunk = group + 4 * (i >> 1);
+                const bool in = mine && chunk * 16 < dim;
+                load_q<TWO>(a.q, base + (in ? chunk * 16 + 8 * (i & 1) : 0),
+                            a.dtype, x[i]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[i][e] = in ? x[i][e] : 0.0f;
+                    sum += x[i][e];
+                    top = fmaxf(top, fabsf(x[i][e]));
+                }
+            }
+            top = over_groups(top, larger);
+            sum = over_groups(sum, add);
+            // an infinity makes the whole head NaN, as a NaN does by itself
+            if (!(top < INFINITY)) sum = NAN;
+            // 2^e with top 2^-e in [2^9, 2^10); below 2^-100 it stays there
+            const int e =
+                max((int)(f32_bits(top) >> 23), 27) - 127 - 9;
+            const float down = ldexpf(1.0f, -e), back = ldexpf(1.0f, e);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float y = x[i][key_channel<KB>(j)] * down;
+                    const _Float16 hi = (_Float16)y;
+                    const _Float16 f = (_Float16)key_factor<KB>(j);
+                    q_hi[i][j] = hi * f;
+                    if constexpr (TWO)
+                        q_lo[i][j] = (_Float16)((y - (float)hi) *
+                                                key_factor<KB>(j));
+                }
+            q_scale = a.scale2 * back;
+            q_sum = a.scale2 * sum;
+        }
+
+        f32x4 o[kOwn];
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) o[j] = f32x4{0, 0, 0, 0};
+        float top = kNone;          // running maximum m of the logits
+        float s_top = 0.0f;         // S: a power of two, above every s and
+                                    // 2^-10 |z| so far
+        float mo = kNone;           // m + log2 S - 7
+        float sum_p = 0.0f, sum_z = 0.0f;
+
+        for (int32_t c = c0; c < c1; ++c) {
+            // ---- logits
+            f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    half8v f;
+                    if constexpr (KB == 8)
+                        f = key_operand<8>(codes.k[s][i >> 1][2 * (i & 1)],
+                                           codes.k[s][i >> 1][2 * (i & 1) + 1]);
+                    else
+                        f = key_operand<4>(codes.k[s][i >> 1][i & 1], 0);
+                    acc[s] = mfma(f, q_hi[i], acc[s]);
+                    if constexpr (TWO) acc[s] = mfma(f, q_lo[i], acc[s]);
+                }
+            const bool more = c + 1 < c1;
+            if (more) load_keys(next);
+
+            // ---- softmax
+            const bool whole = now.token >= span.first &&
+                               now.token + 32 <= span.length && now.there[0] &&
+                               now.there[1];
+            float x[2][4];
+            float big = -INFINITY, s_big = 0.0f, z_big = 0.0f;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t kw = ks[s][i];
+                    bool seen = true;
+                    if (!whole) {
+                        const int32_t t = now.token + 16 * s + 4 * group + i;
+                        seen = now.there[s] && t >= span.first &&
+                               t < span.length;
+                        // rows never written may hold anything
+                        kw = seen ? kw : 0;
+                        vs[s][i] = seen ? vs[s][i] : 0;
+                    }
+                    const float kstep = step_of(kw);
+                    const float koff =
+                        __builtin_fmaf(kstep, kCentreK, offset_of(kw));
+                    x[s][i] = __builtin_fmaf(acc[s][i], kstep * q_scale,
+                                             koff * q_sum);
+                    if (!whole) x[s][i] = seen ? x[s][i] : -INFINITY;
+                    big = fmaxf(big, x[s][i]);
+                    s_big = fmaxf(s_big, step_of(vs[s][i]));
+                    z_big = fmaxf(z_big, fabsf(offset_of(vs[s][i])));
+                }
+            s_big = fmaxf(s_big, z_big * 0x1p-10f);
+            if (__any(big > top + 8.0f || s_big > s_top)) {
+                top = fmaxf(top, over_groups(big, larger));
+                float s_all = over_groups(s_big, larger);
+#pragma unroll
+                for (int d = 1; d < 16; d *= 2)
+                    s_all = fmaxf(s_all, __shfl_xor(s_all, d));
+                // (at least 2^-60: the quantizer's smallest step)
+                const uint32_t e = max(f32_bits(s_all) >> 23, 127u - 61u) + 1;
+                s_top = fmaxf(s_top, bits_f32(e << 23));
+                const float lift =
+                    (float)((int)(f32_bits(s_top) >> 23) - 127 - 7);
+                const float mo_new = top + lift;
+                const float f = __builtin_amdgcn_exp2f(mo - mo_new);
+                mo = mo_new;
+                sum_p *= f;
+                sum_z *= f;
+#pragma unroll
+                for (int j = 0; j < kOwn; ++j) o[j] *= f;
+            }
+            half8v w_hi, w_lo;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(x[s][i] - mo);
+                    const float step = step_of(vs[s][i]);
+                    sum_p += p;
+                    sum_z = __builtin_fmaf(
+                        p, __builtin_fmaf(step, kCentreV, offset_of(vs[s][i])),
+                        sum_z);
+                    const float w = p * step;
+                    const _Float16 hi = (_Float16)w;
+                    w_hi[4 * s + i] = hi;
+                    if constexpr (TWO)
+                        w_lo[4 * s + i] = (_Float16)(w - (float)hi);
+                }
+            if (more) load_steps(next);
+
+            // ---- values
+#pragma unroll
+            for (int j = 0; j < kOwn; j += 4) {
+                uint32_t y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    y[i] = VB == 8 ? codes.v[i][j >> 2]
+                                   : codes.v[i][j >> 3] >> 16 * ((j >> 2) & 1);
+                half8v f[4];
+                value_operands<VB>(y, f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    o[j + e] = mfma(f[e], w_hi, o[j + e]);
+                    if constexpr (TWO) o[j + e] = mfma(f[e], w_lo, o[j + e]);
+                }
+            }
+            if (more) {
+                load_values(next);
+                now = next;
+                next = find(c + 2);
+            }
+        }
+
+        // ---- the four waves' results
+        sum_p = over_groups(sum_p, add);
+        sum_z = over_groups(sum_z, add);
+        if (group == 0) {
+            sm_m[wave][head] = mo;
+            sm_l[wave][head] = sum_p;
+        }
+        // o[j][i] is channel kOwn (4 group + i) + j of this lane's head
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < kOwn; j += 4) {
+                f32x4 r;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    r[e] = __builtin_fmaf(o[j + e][i],
+                                          value_factor<VB>(j + e), sum_z);
+                *reinterpret_cast<f32x4*>(
+                    &sm_o[wave][head][kOwn * (4 * group + i) + j]) = r;
+            }
+        __syncthreads();
+        const bool is_whole = c0 == 0 && c1 == units;
+        float* part = is_whole ? nullptr
+                               : part_of(a, 2 * self + (c0 > 0 ? 0 : 1));
+        const int quads = dim >> 2;
+        for (int n = threadIdx.x; n < heads * quads; n += kThreads) {
+            const int h = n / quads, d = 4 * (n - h * quads);
+            float m = sm_m[0][h];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm_m[w][h]);
+            f32x4 r = {0, 0, 0, 0};
+            float l = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(sm_m[w][h] - m);
+                l = __builtin_fmaf(f, sm_l[w][h], l);
+                const f32x4 y =
+                    *reinterpret_cast<const f32x4*>(&sm_o[w][h][d]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = __builtin_fmaf(f, y[e], r[e]);
+            }
+            if (is_whole) {
+                const int64_t row = (int64_t)seq * a.heads + h0 + h;
+                const bool none = l == 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : r[e] / l;
+                store_out(a.out, row * dim + d, a.dtype, r);
+                if (d == 0 && a.lse)
+                    a.lse[row] = none ? -INFINITY
+                                      : (m + __builtin_amdgcn_logf(l)) * kLn2;
+            } else {
+                *reinterpret_cast<f32x4*>(part + h * dim + d) = r;
+                if (d == 0) {
+                    part[16 * dim + 2 * h] = m;
+                    part[16 * dim + 2 * h + 1] = l;
+                }
+            }
+        }
+        unit += c1 - c0;
+        if (c1 == units && pair + 1 == pairs) {
+            before += units;
+            ++seq;
+        }
+        if (unit < unit_end) __syncthreads();
+    }
+}
+
+// Joins the partial results of a (sequence, query head) that several
+// workgroups share, in the order of the workgroups.
+template <int UNUSED = 0>
+__global__ __launch_bounds__(kThreads) void join_kernel(const Attend a) {
+    __shared__ f32x4 sm_o[kThreads];
+    __shared__ float sm_m[kWaves], sm_l[kThreads];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t seq = blockIdx.x / a.heads;
+    const int32_t h = blockIdx.x - seq * a.heads;
+    const int32_t kvh = h / a.group, in_group = h - kvh * a.group;
+    const int32_t tile16 = in_group / 16, row = in_group - tile16 * 16;
+    const int32_t pairs = a.c.kv_heads * a.head_tiles;
+    const int dim = a.c.dim;
+    int32_t total = 0, before = 0;
+    for (int32_t b = 0; b < a.batch; b += 64) {
+        const int32_t own = units_of(a, b + lane);
+        const int32_t sum = wave_scan(own, lane);
+        if (seq >= b && seq < b + 64)
+            before = total + __builtin_amdgcn_readlane(sum - own, seq - b);
+        total += __builtin_amdgcn_readlane(sum, 63);
+    }
+    total *= pairs;
+    const int32_t units = span_of(a, a.lengths[seq]).units();
+    const int32_t sharers = sharing(a, total);
+    const int32_t u0 = before * pairs + (kvh * a.head_tiles + tile16) * units;
+    const int32_t i0 = range_of(u0, total, sharers);
+    const int32_t i1 = range_of(u0 + units - 1, total, sharers);
+    if (i0 == i1) return;
+    const int32_t parts = i1 - i0 + 1;
+    auto part = [&](int32_t p) {
+        return part_of(a, 2 * (i0 + p) + (p == 0 ? 1 : 0));
+    };
+    // the largest maximum
+    float m = kNone;
+    for (int32_t p = threadIdx.x; p < parts; p += kThreads)
+        m = fmaxf(m, part(p)[16 * dim + 2 * row]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    if (lane == 0) sm_m[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, sm_m[w]);
+    // columns of 4 channels, and rows of threads that take every rows-th part
+    const int quads = dim >> 2;
+    const int rows = kThreads / quads;
+    const int col = threadIdx.x % quads, mine = threadIdx.x / quads;
+    f32x4 r = {0, 0, 0, 0};
+    float l = 0.0f;
+    if (mine < rows)
+        for (int32_t p = mine; p < parts; p += rows) {
+            const float* q = part(p);
+            const float f =
+                __builtin_amdgcn_exp2f(q[16 * dim + 2 * row] - m);
+            l = __builtin_fmaf(f, q[16 * dim + 2 * row + 1], l);
+            const f32x4 y =
+                *reinterpret_cast<const f32x4*>(q + row * dim + 4 * col);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = __builtin_fmaf(f, y[e], r[e]);
+        }
+    sm_o[threadIdx.x] = r;
+    sm_l[threadIdx.x] = l;
+    __syncthreads();
+    if (mine != 0) return;
+    for (int w = 1; w < rows; ++w) {
+        r += sm_o[w * quads + col];
+        l += sm_l[w * quads + col];
+    }
+    const int64_t at = (int64_t)seq * a.heads + h;
+    const bool none = l == 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : r[e] / l;
+    store_out(a.out, at * dim + 4 * col, a.dtype, r);
+    if (col == 0 && a.lse)
+        a.lse[at] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Launches the kernel for DP padded channels (one translation unit each).
+template <int DP>
+hipError_t launch_attend_dp(const Attend& a, hipStream_t st);
+
+}  // namespace bscache
