@@ -103,25 +103,24 @@ __global__ __launch_bounds__(kBlock) void write_kernel(
     const float top = bits == 8 ? 255.0f : 15.0f;
     const float per = bits == 8 ? 1.0f / 255.0f : 1.0f / 15.0f;
     uint32_t slot[STEPS];
-    float x[STEPS][8];
+    Eight<T> in[STEPS];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
         const int64_t t = first + s * kRows + lane / LPR;
         slot[s] = t < g.tokens ? (uint32_t)slots[t] : ~0u;
         if (t < g.tokens && mine)
-            load8<T>(src, t * stride + (int64_t)head * c.dim + channel, x[s]);
+            in[s].load(src, t * stride + (int64_t)head * c.dim + channel);
         else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[s][i] = 0.0f;
+            in[s].clear();
     }
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        float lo = INFINITY, hi = -INFINITY;
+        float x[8], lo = INFINITY, hi = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[s][i] = finite(x[s][i]);
-            lo = fminf(lo, x[s][i]);
-            hi = fmaxf(hi, x[s][i]);
+            x[i] = finite(in[s].get(i));
+            lo = fminf(lo, x[i]);
+            hi = fmaxf(hi, x[i]);
         }
         if (!mine) lo = INFINITY, hi = -INFINITY;
         lo = reduce_row<LPR>(lo, [](float a, float b) { return fminf(a, b); });
@@ -139,7 +138,7 @@ __global__ __launch_bounds__(kBlock) void write_kernel(
             const uint32_t page = c.by_page.div(slot[s]);
             const int64_t row =
                 row_of(c, page, head, slot[s] - page * c.by_page.d);
-            const u32x2 d = codes8(x[s], z, inv, top);
+            const u32x2 d = codes8(x, z, inv, top);
             uint8_t* codes = c.codes[side];
             if (bits == 8)
                 *reinterpret_cast<u32x2*>(codes + row * c.dim + channel) = d;

@@ -16,26 +16,30 @@
 //           tokens 4 g .. + 3 of both halves, and lane l loads those tokens'
 //           codes.  No weight ever moves between lanes.
 //
-// Codes become float16 without conversions: 0x6400 | c is 1024 + c, and one
-// packed subtraction of 1024 + centre (128 or 8) gives the centred code c',
-// exactly.  4-bit codes in the second nibble of a byte stay there (1024 + 16
-// c): their products carry a factor of 16, which the queries (keys) or the
-// final outputs (values) of those channels take back.  With the centre in the
-// offset, value = s c' + (z + centre s), so
-//   logit = scale (s (q . c') + (z + centre s) sum q)
-//   out   = (sum_t w_t c'_t + sum_t p_t (z_t + centre s_t)) / sum_t p_t
-// with w = p s.
+// Codes become float16 without conversions.  For 16-bit calls a code's own bits
+// are the operand: as a float16 they are the subnormal c 2^-24, which the
+// matrix unit multiplies exactly (one byte permutation or mask for two codes).
+// 4-bit codes in the second nibble of a byte stay there and count 16 c; the
+// queries (keys) or the final outputs (values) of those channels take the 16
+// back.  float32 calls centre the codes: 0x6400 | c is 1024 + c, and one packed
+// subtraction of 1024 + centre (128 or 8) gives c' = c - centre exactly, so
+// that sums do not grow by the offset and cancel again.  With z' = z + centre s
+// (centre 0 where the codes are not centred) a value is s c' + z', and
+//   logit = scale (s (q . c') + z' sum q)
+//   out   = (sum_t w_t c'_t + sum_t p_t z'_t) / sum_t p_t,   w = p s.
 //
-// Roundings: q is scaled by a power of two to below 2^10 and rounded to
+// Roundings: q is scaled by a power of two to below 2^14 and rounded to
 // float16: bfloat16 and float16 values keep all their bits, but for what lies
-// below 2^-30 of the row's largest; float32 queries take a second float16 for the
-// rest (22 bits together), a second MFMA into the same accumulator.  w is
-// rounded to float16 (2^-12 relative, within the 2^-12 and 2^-9 of the output
-// types; float32 calls take a second float16 too).  w = 2^7 (p / 2^m) (s / S)
-// with m the running maximum and S a power of two above every s, and 2^-10 |z|,
-// so far (z far beyond s is a row of nearly equal values, whose sums p z would
-// leave binary32); m may lag by 2^8, so w stays below 2^15 and keeps its full
-// precision down to 2^-21 of the largest weight.  Everything else is float32.
+// below 2^-30 of the row's largest; float32 queries take a second float16 for
+// the rest (22 bits together), a second MFMA into the same accumulator.  w is
+// rounded to float16 for bfloat16 calls: 2^-12 of w c, 3 times the spread of
+// the values where codes are not centred, against the output's own 2^-9.
+// float16 and float32 calls take a second float16 for the rest of w.
+// w = 2^7 (p / 2^m) (s / S) with m the running maximum and S a power of two
+// above every s, and 2^-10 |z|, so far (z far beyond s is a row of nearly equal
+// values, whose sums p z would leave binary32); m may lag by 2^8, so w stays
+// below 2^15 and keeps its full precision down to 2^-21 of the largest weight.
+// Everything else is float32.
 //
 // Sharing: the units of all (sequence, head tile) pairs are numbered in one
 // row, and workgroup i of n takes units [i U / n, (i + 1) U / n): every
@@ -75,27 +79,41 @@ __device__ __forceinline__ Span span_of(const Attend& a, int32_t length) {
     return s;
 }
 
-// Inclusive sum over the lanes of a wave up to this one.
-__device__ __forceinline__ int32_t wave_scan(int32_t v, int lane) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int32_t up = __shfl_up(v, d);
-        v += lane >= d ? up : 0;
-    }
-    return v;
+// Inclusive sum over the lanes of a wave up to this one: within rows of 16
+// lanes, then the rows' sums passed on (DPP moves; lanes without a source add
+// 0).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int32_t scan_step(int32_t v) {
+    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int32_t wave_scan(int32_t v) {
+    v = scan_step<0x111, 0xF>(v);       // row_shr 1, 2, 4, 8
+    v = scan_step<0x112, 0xF>(v);
+    v = scan_step<0x114, 0xF>(v);
+    v = scan_step<0x118, 0xF>(v);
+    v = scan_step<0x142, 0xA>(v);       // row_bcast 15 into rows 1 and 3
+    return scan_step<0x143, 0xC>(v);    // row_bcast 31 into rows 2 and 3
 }
 
 __device__ __forceinline__ int32_t units_of(const Attend& a, int32_t b) {
     return b < a.batch ? span_of(a, a.lengths[b]).units() : 0;
 }
 
-// Units of all sequences for one head tile.
-__device__ __forceinline__ int32_t all_units(const Attend& a, int lane) {
+// Units of the sequences from 64 on.
+__device__ __forceinline__ int32_t units_behind(const Attend& a, int lane) {
     int32_t total = 0;
-    for (int32_t b = 0; b < a.batch; b += 64)
-        total += __builtin_amdgcn_readlane(wave_scan(units_of(a, b + lane), lane),
+    for (int32_t b = 64; b < a.batch; b += 64)
+        total += __builtin_amdgcn_readlane(wave_scan(units_of(a, b + lane)),
                                            63);
     return total;
+}
+
+// A word of a table that the kernel only reads, at a place that is the same
+// for the whole wave: a scalar load, whose wait does not wait for the codes
+// in flight.
+__device__ __forceinline__ int32_t uniform_load(const int32_t* p, int64_t at) {
+    typedef const __attribute__((address_space(4))) int32_t* Constant;
+    return ((Constant)(uintptr_t)p)[at];
 }
 
 // The workgroups that share u units: every one of them has at least one.
@@ -125,25 +143,39 @@ __device__ __forceinline__ uint32_t minus(uint32_t pair, _Float16 bias) {
                               __builtin_bit_cast(half2v, pair) - b);
 }
 
+// Two 4-bit codes, 16 bits apart: nibble N (0, 1: of the low byte) of x.
+template <int N, bool CENTRED>
+__device__ __forceinline__ uint32_t nibble_pair(uint32_t x) {
+    const uint32_t c = x & (N ? 0x00F000F0u : 0x000F000Fu);
+    if constexpr (!CENTRED) return c;
+    return minus(c | 0x64006400u, (_Float16)(N ? 1152.0f : 1032.0f));
+}
+// Two 8-bit codes: bytes A and B of the pair (hi, lo), lo's are 0..3.
+template <int A, int B, bool CENTRED>
+__device__ __forceinline__ uint32_t byte_pair(uint32_t hi, uint32_t lo) {
+    const uint32_t c =
+        __builtin_amdgcn_perm(hi, lo, 0x0C000C00u | B << 16 | A);
+    if constexpr (!CENTRED) return c;
+    return minus(c | 0x64006400u, (_Float16)1152.0f);
+}
+
 // Channel-major operand of the keys: 8 codes of one token as 4 words of two
 // float16 each.  8 bits: x, y hold 4 codes each, in order.  4 bits: x holds 8
 // codes; the pairs are (0,4) (1,5) (2,6) (3,7), the second and fourth times 16.
-template <int BITS>
+template <int BITS, bool CENTRED>
 __device__ __forceinline__ half8v key_operand(uint32_t x, uint32_t y) {
     u32x4 f;
     if constexpr (BITS == 8) {
-        f[0] = __builtin_amdgcn_perm(0x64646464u, x, 0x04010400u);
-        f[1] = __builtin_amdgcn_perm(0x64646464u, x, 0x04030402u);
-        f[2] = __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u);
-        f[3] = __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = minus(f[i], (_Float16)1152.0f);
+        f[0] = byte_pair<0, 1, CENTRED>(x, x);
+        f[1] = byte_pair<2, 3, CENTRED>(x, x);
+        f[2] = byte_pair<0, 1, CENTRED>(y, y);
+        f[3] = byte_pair<2, 3, CENTRED>(y, y);
     } else {
         const uint32_t h = x >> 8;
-        f[0] = minus((x & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f);
-        f[1] = minus((x & 0x00F000F0u) | 0x64006400u, (_Float16)1152.0f);
-        f[2] = minus((h & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f);
-        f[3] = minus((h & 0x00F000F0u) | 0x64006400u, (_Float16)1152.0f);
+        f[0] = nibble_pair<0, CENTRED>(x);
+        f[1] = nibble_pair<1, CENTRED>(x);
+        f[2] = nibble_pair<0, CENTRED>(h);
+        f[3] = nibble_pair<1, CENTRED>(h);
     }
     return __builtin_bit_cast(half8v, f);
 }
@@ -160,7 +192,7 @@ __device__ __forceinline__ constexpr float key_factor(int e) {
 // Token-major operands of the values: from 4 codes of each of 8 tokens (8
 // bits: a word each; 4 bits: the low half of a word each) one operand for each
 // of the 4 channels; of 4-bit codes channels 1 and 3 are times 16.
-template <int BITS>
+template <int BITS, bool CENTRED>
 __device__ __forceinline__ void value_operands(const uint32_t (&x)[8],
                                                half8v (&f)[4]) {
     u32x4 r[4];
@@ -168,22 +200,17 @@ __device__ __forceinline__ void value_operands(const uint32_t (&x)[8],
     for (int p = 0; p < 4; ++p) {
         const uint32_t a = x[2 * p], b = x[2 * p + 1];
         if constexpr (BITS == 8) {
-            const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x05010400u);
-            const uint32_t hi = __builtin_amdgcn_perm(b, a, 0x07030602u);
-            r[0][p] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u);
-            r[1][p] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u);
-            r[2][p] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u);
-            r[3][p] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                r[i][p] = minus(r[i][p], (_Float16)1152.0f);
+            r[0][p] = byte_pair<0, 4, CENTRED>(b, a);
+            r[1][p] = byte_pair<1, 5, CENTRED>(b, a);
+            r[2][p] = byte_pair<2, 6, CENTRED>(b, a);
+            r[3][p] = byte_pair<3, 7, CENTRED>(b, a);
         } else {
             const uint32_t v = __builtin_amdgcn_perm(b, a, 0x05040100u);
             const uint32_t h = v >> 8;
-            r[0][p] = minus((v & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f);
-            r[1][p] = minus((v & 0x00F000F0u) | 0x64006400u, (_Float16)1152.0f);
-            r[2][p] = minus((h & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f);
-            r[3][p] = minus((h & 0x00F000F0u) | 0x64006400u, (_Float16)1152.0f);
+            r[0][p] = nibble_pair<0, CENTRED>(v);
+            r[1][p] = nibble_pair<1, CENTRED>(v);
+            r[2][p] = nibble_pair<0, CENTRED>(h);
+            r[3][p] = nibble_pair<1, CENTRED>(h);
         }
     }
 #pragma unroll
@@ -207,13 +234,6 @@ __device__ __forceinline__ float over_groups(float v, F f) {
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 
-template <bool TWO>
-__device__ __forceinline__ void load_q(const void* q, int64_t at, int dtype,
-                                       float (&x)[8]) {
-    if constexpr (TWO) load8<kF32>(q, at, x);
-    else if (dtype == kF16) load8<kF16>(q, at, x);
-    else load8<kBF16>(q, at, x);
-}
 __device__ __forceinline__ void store_out(void* out, int64_t at, int dtype,
                                           f32x4 v) {
     if (dtype == kF32) {
@@ -241,40 +261,55 @@ struct Codes {
     uint32_t v[8][kValueWords];
 };
 
-// N words from a 4 N-byte aligned address (2 bytes where HALF).
+// The rows of half a tile as a buffer: the base stays in scalar registers, a
+// lane's offset in one vector register, and nothing behind the rows can be
+// read.
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+__device__ __forceinline__ Rsrc rows_buffer(const void* base, int64_t at,
+                                            int32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(static_cast<const uint8_t*>(base)) + at, (short)0,
+        bytes, 0x00020000);   // 32-bit data format
+}
+// N words from a 4 N-byte aligned offset.
 template <int N>
-__device__ __forceinline__ void load_words(const uint8_t* p,
+__device__ __forceinline__ void load_words(Rsrc rows, uint32_t at,
                                            uint32_t (&w)[N]) {
     if constexpr (N == 1) {
-        w[0] = *reinterpret_cast<const uint32_t*>(p);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b32(rows, at, 0, 0);
     } else if constexpr (N == 2) {
-        const u32x2 t = *reinterpret_cast<const u32x2*>(p);
+        const u32x2 t = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, 0));
         w[0] = t[0], w[1] = t[1];
     } else {
         static_assert(N == 4);
-        const u32x4 t = *reinterpret_cast<const u32x4*>(p);
+        const u32x4 t = __builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, 0));
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = t[i];
     }
 }
 
 // Where the two halves of a wave's tile lie: the row of each half's first
-// token, and whether its page is one of the cache.  Half a tile never leaves
-// a page (pages are multiples of 16 tokens).
+// token, and the end of its visible tokens (0 where its page is none of the
+// cache).  Half a tile never leaves a page (pages are multiples of 16 tokens).
 struct Tile {
     int32_t token;          // first token
     int64_t row[2];
-    bool there[2];
+    int32_t end[2];
 };
 
-template <int DP, int KB, int VB, bool TWO>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
+template <int DP, int KB, int VB, int T>
+__global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
     const Attend a) {
     using C = Codes<DP, KB, VB>;
     constexpr int kSteps = DP / 32;             // MFMAs of the logits
     constexpr int kOwn = C::kOwn;
-    constexpr float kCentreK = KB == 8 ? 128.0f : 8.0f;
-    constexpr float kCentreV = VB == 8 ? 128.0f : 8.0f;
+    constexpr bool kTwoQ = T == kF32, kTwoW = T != kBF16, kCentred = T == kF32;
+    constexpr float kCentreK = !kCentred ? 0.0f : KB == 8 ? 128.0f : 8.0f;
+    constexpr float kCentreV = !kCentred ? 0.0f : VB == 8 ? 128.0f : 8.0f;
+    // what a code's bits stand for as float16
+    constexpr float kCode = kCentred ? 1.0f : 0x1p24f;
     __shared__ float sm_o[kWaves][16][DP + 4];
     __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
 
@@ -285,18 +320,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
     const int32_t pairs = a.c.kv_heads * a.head_tiles;
 
     // this workgroup's units and the sequence of the first
-    const int32_t total = all_units(a, lane) * pairs;
+    int32_t own = units_of(a, lane);
+    int32_t sum = wave_scan(own);
+    const int32_t total =
+        (__builtin_amdgcn_readlane(sum, 63) + units_behind(a, lane)) * pairs;
     const int32_t sharers = sharing(a, total);
     const int32_t self = blockIdx.x;
     if (self >= sharers) return;
     int32_t unit = range_start(self, total, sharers);
     const int32_t unit_end = range_start(self + 1, total, sharers);
     int32_t seq = 0, before = 0;     // units before seq, in one head tile
-    for (int32_t b = 0;; b += 64) {
-        const int32_t own = units_of(a, b + lane);
-        const int32_t sum = wave_scan(own, lane);
+    for (int32_t b = 0;;) {
         const int32_t all = __builtin_amdgcn_readlane(sum, 63);
-        // (units of 64 sequences times pairs stay within total)
         if (unit < (before + all) * pairs) {
             const uint64_t past = __ballot((before + sum) * pairs > unit);
             const int at = __builtin_ctzll(past);
@@ -305,8 +340,10 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
             break;
         }
         before += all;
+        b += 64;
+        own = units_of(a, b + lane);
+        sum = wave_scan(own);
     }
-    seq = __builtin_amdgcn_readfirstlane(seq);
 
     // lane offsets, in bytes, of the codes within 16 rows; lanes behind the
     // last channel read their row's first codes (their products are dropped)
@@ -321,7 +358,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
         4 * group * v_row + (head * kOwn < dim ? head * kOwn * VB / 8 : 0);
 
     while (unit < unit_end) {
-        const Span span = span_of(a, a.lengths[seq]);
+        const Span span = span_of(a, uniform_load(a.lengths, seq));
         const int32_t units = span.units();
         const int32_t rel = unit - before * pairs;
         const int32_t pair = rel / units;
@@ -336,8 +373,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
 
         // ---- tiles and their loads
         C codes;
-        u32x4 ks[2], vs[2];
-        const int32_t* table = a.table + (int64_t)seq * a.max_pages;
+        uint32_t ks[2][4], vs[2][4];
+        const int64_t table = (int64_t)seq * a.max_pages;
         auto find = [&](int32_t c) {
             Tile t;
             t.token = span.start() + c * kUnit + wave * 32;
@@ -346,92 +383,109 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
                 const int32_t at = t.token + 16 * s;
                 const bool in = at < span.length && c < c1;
                 const uint32_t p = in ? a.c.by_page.div(at) : 0;
-                const uint32_t page = table[p];
-                t.there[s] = in && page < a.c.pages;
-                t.row[s] = t.there[s]
-                    ? row_of(a.c, page, kvh, at - p * a.c.by_page.d)
-                    : row_of(a.c, 0, kvh, 0);
+                const uint32_t page = uniform_load(a.table, table + p);
+                const bool there = in && page < a.c.pages;
+                t.end[s] = there ? span.length : 0;
+                t.row[s] = row_of(a.c, there ? page : 0, kvh,
+                                  there ? at - p * a.c.by_page.d : 0);
             }
             return t;
         };
         auto load_keys = [&](const Tile& t) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const uint8_t* base = a.c.codes[0] + t.row[s] * k_row;
+                const Rsrc rows =
+                    rows_buffer(a.c.codes[0], t.row[s] * k_row, 16 * k_row);
 #pragma unroll
                 for (int j = 0; j < C::kChunks; ++j)
-                    load_words(base + k_at[j], codes.k[s][j]);
+                    load_words(rows, k_at[j], codes.k[s][j]);
             }
         };
         auto load_steps = [&](const Tile& t) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                ks[s] = *reinterpret_cast<const u32x4*>(
-                    a.c.steps[0] + t.row[s] + 4 * group);
-                vs[s] = *reinterpret_cast<const u32x4*>(
-                    a.c.steps[1] + t.row[s] + 4 * group);
+                load_words(rows_buffer(a.c.steps[0], t.row[s] * 4, 64),
+                           16 * group, ks[s]);
+                load_words(rows_buffer(a.c.steps[1], t.row[s] * 4, 64),
+                           16 * group, vs[s]);
             }
         };
         auto load_values = [&](const Tile& t) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint8_t* p = a.c.codes[1] + t.row[i >> 2] * v_row + v_at +
-                                   (i & 3) * v_row;
-                if constexpr (kOwn * VB < 32)
-                    codes.v[i][0] = *reinterpret_cast<const uint16_t*>(p);
-                else
-                    load_words(p, codes.v[i]);
+            for (int s = 0; s < 2; ++s) {
+                const Rsrc rows =
+                    rows_buffer(a.c.codes[1], t.row[s] * v_row, 16 * v_row);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t at = v_at + i * v_row;
+                    if constexpr (kOwn * VB < 32)
+                        codes.v[4 * s + i][0] =
+                            __builtin_amdgcn_raw_buffer_load_b16(rows, at, 0,
+                                                                 0);
+                    else
+                        load_words(rows, at, codes.v[4 * s + i]);
+                }
             }
         };
+
+        // the queries of this lane's head, loaded ahead of the codes and kept
+        // as they are stored until they become operands
+        Eight<T> qx[kSteps];
+        const bool mine = head < heads;
+        {
+            const int64_t base =
+                seq * a.q_stride + (int64_t)(h0 + (mine ? head : 0)) * dim;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int chunk = group + 4 * (i >> 1);
+                qx[i].load(a.q, base + (chunk * 16 < dim
+                                            ? chunk * 16 + 8 * (i & 1) : 0));
+            }
+        }
         Tile now = find(c0);
         load_keys(now);
         load_steps(now);
         load_values(now);
         Tile next = find(c0 + 1);
 
-        // ---- the queries of this lane's head as B operands
-        half8v q_hi[kSteps], q_lo[TWO ? kSteps : 1];
-        float q_scale, q_sum;       // of logits in units of log2
+        // ---- the queries as B operands
+        half8v q_hi[kSteps], q_lo[kTwoQ ? kSteps : 1];
+        // a logit in units of log2 is (s (q' . c') + z' q_sum) q_scale
+        float q_scale, q_sum;
         {
-            float x[kSteps][8], top = 0.0f, sum = 0.0f;
-            const int64_t base = seq * a.q_stride +
-                                 (int64_t)(h0 + (head < heads ? head : 0)) * dim;
-            const bool mine = head < heads;
+            float top = 0.0f, sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const int chunk = group + 4 * (i >> 1);
-                const bool in = mine && chunk * 16 < dim;
-                load_q<TWO>(a.q, base + (in ? chunk * 16 + 8 * (i & 1) : 0),
-                            a.dtype, x[i]);
+                if (!mine || (group + 4 * (i >> 1)) * 16 >= dim) qx[i].clear();
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[i][e] = in ? x[i][e] : 0.0f;
-                    sum += x[i][e];
-                    top = fmaxf(top, fabsf(x[i][e]));
+                    const float x = qx[i].get(e);
+                    sum += x;
+                    top = fmaxf(top, fabsf(x));
                 }
             }
             top = over_groups(top, larger);
             sum = over_groups(sum, add);
             // an infinity makes the whole head NaN, as a NaN does by itself
             if (!(top < INFINITY)) sum = NAN;
-            // 2^e with top 2^-e in [2^9, 2^10); below 2^-100 it stays there
-            const int e =
-                max((int)(f32_bits(top) >> 23), 27) - 127 - 9;
-            const float down = ldexpf(1.0f, -e), back = ldexpf(1.0f, e);
+            // 2^-e brings the largest into [2^13, 2^14); tiny rows stay below
+            const int e = max((int)(f32_bits(top) >> 23), 27) - 127 - 13;
+            // (the sign of the scale goes into q: q_scale is not negative)
+            const float down = copysignf(ldexpf(1.0f, -e), a.scale2);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float y = x[i][key_channel<KB>(j)] * down;
+                    const float y = qx[i].get(key_channel<KB>(j)) * down;
                     const _Float16 hi = (_Float16)y;
-                    const _Float16 f = (_Float16)key_factor<KB>(j);
-                    q_hi[i][j] = hi * f;
-                    if constexpr (TWO)
+                    q_hi[i][j] = hi * (_Float16)key_factor<KB>(j);
+                    if constexpr (kTwoQ)
                         q_lo[i][j] = (_Float16)((y - (float)hi) *
                                                 key_factor<KB>(j));
                 }
-            q_scale = a.scale2 * back;
-            q_sum = a.scale2 * sum;
+            // (above 0, so that a masked -inf stays one)
+            q_scale = fmaxf(fabsf(a.scale2) * ldexpf(kCode, e), 1e-30f);
+            q_sum = sum * down * (1.0f / kCode);
         }
 
         f32x4 o[kOwn];
@@ -450,48 +504,58 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
+                    const uint32_t(&w)[C::kKeyWords] = codes.k[s][i >> 1];
                     half8v f;
                     if constexpr (KB == 8)
-                        f = key_operand<8>(codes.k[s][i >> 1][2 * (i & 1)],
-                                           codes.k[s][i >> 1][2 * (i & 1) + 1]);
+                        f = key_operand<8, kCentred>(w[2 * (i & 1)],
+                                                     w[2 * (i & 1) + 1]);
                     else
-                        f = key_operand<4>(codes.k[s][i >> 1][i & 1], 0);
+                        f = key_operand<4, kCentred>(w[i & 1], 0);
                     acc[s] = mfma(f, q_hi[i], acc[s]);
-                    if constexpr (TWO) acc[s] = mfma(f, q_lo[i], acc[s]);
+                    if constexpr (kTwoQ) acc[s] = mfma(f, q_lo[i], acc[s]);
                 }
             const bool more = c + 1 < c1;
             if (more) load_keys(next);
 
             // ---- softmax
             const bool whole = now.token >= span.first &&
-                               now.token + 32 <= span.length && now.there[0] &&
-                               now.there[1];
+                               now.token + 16 <= now.end[0] &&
+                               now.token + 32 <= now.end[1];
+            if (!whole) {
+                // tokens that are not seen: a logit of 1 * -inf + 0, no
+                // value.  (Rows never written may hold anything.)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int32_t t = now.token + 16 * s + 4 * group + i;
+                        const bool seen = (t >= span.first) & (t < now.end[s]);
+                        ks[s][i] = seen ? ks[s][i] : 0x3F80u;
+                        vs[s][i] = seen ? vs[s][i] : 0;
+                        acc[s][i] = seen ? acc[s][i] : -INFINITY;
+                    }
+            }
             float x[2][4];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float step = step_of(ks[s][i]);
+                    float z = offset_of(ks[s][i]);
+                    if constexpr (kCentred)
+                        z = __builtin_fmaf(step, kCentreK, z);
+                    x[s][i] = __builtin_fmaf(step, acc[s][i], z * q_sum);
+                }
             float big = -INFINITY, s_big = 0.0f, z_big = 0.0f;
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    uint32_t kw = ks[s][i];
-                    bool seen = true;
-                    if (!whole) {
-                        const int32_t t = now.token + 16 * s + 4 * group + i;
-                        seen = now.there[s] && t >= span.first &&
-                               t < span.length;
-                        // rows never written may hold anything
-                        kw = seen ? kw : 0;
-                        vs[s][i] = seen ? vs[s][i] : 0;
-                    }
-                    const float kstep = step_of(kw);
-                    const float koff =
-                        __builtin_fmaf(kstep, kCentreK, offset_of(kw));
-                    x[s][i] = __builtin_fmaf(acc[s][i], kstep * q_scale,
-                                             koff * q_sum);
-                    if (!whole) x[s][i] = seen ? x[s][i] : -INFINITY;
                     big = fmaxf(big, x[s][i]);
                     s_big = fmaxf(s_big, step_of(vs[s][i]));
                     z_big = fmaxf(z_big, fabsf(offset_of(vs[s][i])));
                 }
+            big *= q_scale;
             s_big = fmaxf(s_big, z_big * 0x1p-10f);
             if (__any(big > top + 8.0f || s_big > s_top)) {
                 top = fmaxf(top, over_groups(big, larger));
@@ -517,16 +581,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(x[s][i] - mo);
+                    const float p = __builtin_amdgcn_exp2f(
+                        __builtin_fmaf(x[s][i], q_scale, -mo));
                     const float step = step_of(vs[s][i]);
+                    float z = offset_of(vs[s][i]);
+                    if constexpr (kCentred)
+                        z = __builtin_fmaf(step, kCentreV, z);
                     sum_p += p;
-                    sum_z = __builtin_fmaf(
-                        p, __builtin_fmaf(step, kCentreV, offset_of(vs[s][i])),
-                        sum_z);
+                    sum_z = __builtin_fmaf(p, z, sum_z);
                     const float w = p * step;
                     const _Float16 hi = (_Float16)w;
                     w_hi[4 * s + i] = hi;
-                    if constexpr (TWO)
+                    if constexpr (kTwoW)
                         w_lo[4 * s + i] = (_Float16)(w - (float)hi);
                 }
             if (more) load_steps(next);
@@ -540,11 +606,11 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
                     y[i] = VB == 8 ? codes.v[i][j >> 2]
                                    : codes.v[i][j >> 3] >> 16 * ((j >> 2) & 1);
                 half8v f[4];
-                value_operands<VB>(y, f);
+                value_operands<VB, kCentred>(y, f);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     o[j + e] = mfma(f[e], w_hi, o[j + e]);
-                    if constexpr (TWO) o[j + e] = mfma(f[e], w_lo, o[j + e]);
+                    if constexpr (kTwoW) o[j + e] = mfma(f[e], w_lo, o[j + e]);
                 }
             }
             if (more) {
@@ -569,8 +635,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
                 f32x4 r;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    r[e] = __builtin_fmaf(o[j + e][i],
-                                          value_factor<VB>(j + e), sum_z);
+                    r[e] = __builtin_fmaf(
+                        o[j + e][i], value_factor<VB>(j + e) * kCode, sum_z);
                 *reinterpret_cast<f32x4*>(
                     &sm_o[wave][head][kOwn * (4 * group + i) + j]) = r;
             }
@@ -600,7 +666,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 3) void attend_kernel(
                 const bool none = l == 0.0f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : r[e] / l;
-                store_out(a.out, row * dim + d, a.dtype, r);
+                store_out(a.out, row * dim + d, T, r);
                 if (d == 0 && a.lse)
                     a.lse[row] = none ? -INFINITY
                                       : (m + __builtin_amdgcn_logf(l)) * kLn2;
@@ -638,7 +704,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a) {
     int32_t total = 0, before = 0;
     for (int32_t b = 0; b < a.batch; b += 64) {
         const int32_t own = units_of(a, b + lane);
-        const int32_t sum = wave_scan(own, lane);
+        const int32_t sum = wave_scan(own);
         if (seq >= b && seq < b + 64)
             before = total + __builtin_amdgcn_readlane(sum - own, seq - b);
         total += __builtin_amdgcn_readlane(sum, 63);

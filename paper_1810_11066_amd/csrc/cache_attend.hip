@@ -10,7 +10,9 @@ template <> hipError_t launch_attend_dp<256>(const Attend&, hipStream_t);
 
 int attend_blocks(const Attend& a, int64_t max_units) {
     // as many workgroups as run at once
-    const int64_t most = (int64_t)device_cus() * (a.c.dim > 128 ? 2 : 3);
+    const int dp = a.c.dim > 128 ? 256 : a.c.dim > 64 ? 128 : 64;
+    const int64_t most =
+        (int64_t)device_cus() * attend_waves(dp, a.dtype);
     const int64_t n = max_units < most ? max_units : most;
     return (int)(n < 1 ? 1 : n);
 }

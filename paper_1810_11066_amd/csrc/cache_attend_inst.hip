@@ -1,19 +1,22 @@
-// The attention kernels for BS_DP padded channels: key and value widths, and
-// float32 (two float16 terms) or 16-bit calls.
+// The attention kernels for BS_DP padded channels: every pair of key and value
+// widths, every type.
 #include "cache_attend.h"
 
 namespace bscache {
 namespace {
 
+template <int DP, int KB, int VB, int T>
+hipError_t go(const Attend& a, hipStream_t st) {
+    hipLaunchKernelGGL((attend_kernel<DP, KB, VB, T>), dim3(a.blocks),
+                       dim3(kThreads), 0, st, a);
+    return hipGetLastError();
+}
+
 template <int DP, int KB, int VB>
 hipError_t go(const Attend& a, hipStream_t st) {
-    if (a.dtype == kF32)
-        hipLaunchKernelGGL((attend_kernel<DP, KB, VB, true>), dim3(a.blocks),
-                           dim3(kThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL((attend_kernel<DP, KB, VB, false>), dim3(a.blocks),
-                           dim3(kThreads), 0, st, a);
-    return hipGetLastError();
+    return a.dtype == kF32   ? go<DP, KB, VB, kF32>(a, st)
+           : a.dtype == kF16 ? go<DP, KB, VB, kF16>(a, st)
+                             : go<DP, KB, VB, kBF16>(a, st);
 }
 
 }  // namespace

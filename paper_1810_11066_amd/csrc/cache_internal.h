@@ -78,23 +78,27 @@ __device__ __forceinline__ void unpack2(uint32_t w, float& a, float& b) {
     }
 }
 
-// Eight consecutive elements as float32.
+// Eight consecutive elements, in registers as they are stored.
 template <int T>
-__device__ __forceinline__ void load8(const void* base, int64_t at,
-                                      float (&x)[8]) {
-    if constexpr (T == kF32) {
-        const f32x4* p = reinterpret_cast<const f32x4*>(
-            static_cast<const float*>(base) + at);
-        const f32x4 lo = p[0], hi = p[1];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = lo[i], x[4 + i] = hi[i];
-    } else {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(
-            static_cast<const uint16_t*>(base) + at);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) unpack2<T>(w[i], x[2 * i], x[2 * i + 1]);
+struct Eight {
+    u32x4 w[T == kF32 ? 2 : 1];
+    __device__ __forceinline__ void load(const void* base, int64_t at) {
+        const u32x4* p = reinterpret_cast<const u32x4*>(
+            static_cast<const uint8_t*>(base) + at * (T == kF32 ? 4 : 2));
+        w[0] = p[0];
+        if constexpr (T == kF32) w[1] = p[1];
     }
-}
+    __device__ __forceinline__ void clear() {
+        w[0] = u32x4{0, 0, 0, 0};
+        if constexpr (T == kF32) w[1] = u32x4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (T == kF32) return bits_f32(w[i >> 2][i & 3]);
+        float a, b;
+        unpack2<T>(w[0][i >> 1], a, b);
+        return i & 1 ? b : a;
+    }
+};
 
 // ---- launchers (each returns hipSuccess or the launch error) ---------------
 
@@ -124,6 +128,12 @@ struct Attend {
     float scale2;             // scale log2(e)
     int32_t blocks;           // workgroups that share the units
 };
+
+// Waves of a SIMD that the attention kernel for dp padded channels and a type
+// leaves room for (its registers), and workgroups of a CU.
+constexpr int attend_waves(int dp, int dtype) {
+    return (dp == 64 ? 4 : dp == 128 ? 3 : 2) - (dtype == kF32 ? 1 : 0);
+}
 
 // Tokens of a unit: what the waves of a workgroup take in one step.
 constexpr int kUnit = 128;
