@@ -520,8 +520,7 @@ bscache_status bscache_read(const bscache_pages* cache, const int32_t* slots,
 static bscache_status check_attend(const bscache_pages* cache,
                                    const bscache_attend_params* p,
                                    bscache::Attend* a, Range* range,
-                                   bool pointers, bool* join,
-                                   int64_t* workspace) {
+                                   bool pointers, int64_t* workspace) {
     bscache_status st;
     if ((st = check_cache(cache, &a->c, range, pointers)) != BSCACHE_OK)
         return st;
@@ -561,14 +560,13 @@ static bscache_status check_attend(const bscache_pages* cache,
         span = (int64_t)p->window + 15;
     const int64_t units = (span + bscache::kUnit - 1) / bscache::kUnit;
     const int64_t pairs = (int64_t)a->c.kv_heads * a->head_tiles;
-    if ((int64_t)p->batch * pairs > INT32_MAX / (2 * units) ||
+    if ((int64_t)p->batch * pairs > INT32_MAX / (2 * (units + 8)) ||
         (int64_t)p->batch * p->heads > INT32_MAX)
         return fail(BSCACHE_ERR_UNSUPPORTED,
                     "more than 2^31 - 1 tiles of 64 tokens, or rows");
-    a->blocks = bscache::attend_blocks(*a, p->batch * pairs * units);
-    *join = units > 1;
-    *workspace = units > 1 ? (int64_t)a->blocks * 2 * 16 * (a->c.dim + 2) * 4
-                           : 0;
+    bscache::plan_attend(*a, units);
+    *workspace =
+        a->whole ? 0 : (int64_t)a->blocks * 2 * 16 * (a->c.dim + 2) * 4;
     return BSCACHE_OK;
 }
 
@@ -577,9 +575,7 @@ bscache_status bscache_attend_workspace(const bscache_pages* cache,
                                         int64_t* bytes) {
     if (!bytes) return fail(BSCACHE_ERR_INVALID_ARG, "bytes is NULL");
     bscache::Attend a;
-    bool join;
-    const bscache_status st =
-        check_attend(cache, p, &a, nullptr, false, &join, bytes);
+    const bscache_status st = check_attend(cache, p, &a, nullptr, false, bytes);
     return st == BSCACHE_OK ? ok() : st;
 }
 
@@ -592,10 +588,8 @@ bscache_status bscache_attend(const bscache_pages* cache,
     bscache_status st;
     bscache::Attend a;
     Range in[7];
-    bool join;
     int64_t need;
-    if ((st = check_attend(cache, p, &a, in, true, &join, &need)) !=
-        BSCACHE_OK)
+    if ((st = check_attend(cache, p, &a, in, true, &need)) != BSCACHE_OK)
         return st;
     if ((st = check_ptr(q, "q")) != BSCACHE_OK) return st;
     if ((st = check_ptr(table, "table")) != BSCACHE_OK) return st;
@@ -625,7 +619,7 @@ bscache_status bscache_attend(const bscache_pages* cache,
     a.out = out;
     a.lse = lse;
     a.parts = static_cast<float*>(workspace);
-    return from_hip(bscache::launch_attend(a, join, (hipStream_t)stream),
+    return from_hip(bscache::launch_attend(a, (hipStream_t)stream),
                     "bscache_attend launch");
 }
 

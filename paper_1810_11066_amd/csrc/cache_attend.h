@@ -41,13 +41,18 @@
 // below 2^15 and keeps its full precision down to 2^-21 of the largest weight.
 // Everything else is float32.
 //
-// Sharing: the units of all (sequence, head tile) pairs are numbered in one
-// row, and workgroup i of n takes units [i U / n, (i + 1) U / n): every
-// workgroup has the same work whatever the lengths.  U depends on the lengths,
-// which only the device knows; each workgroup computes it from them.  A
-// workgroup whose range covers a pair whole writes its output; otherwise it
-// leaves a partial result -- at most two, at the ends of its range -- which
-// join_kernel adds in the order of the workgroups.
+// Sharing: the units of all (sequence, head tile) pairs are numbered in one row
+// of places, and workgroup i of n takes the places [i U / n, (i + 1) U / n):
+// every workgroup has the same work whatever the lengths.  U depends on the
+// lengths, which only the device knows; each workgroup computes it from them.
+// A workgroup whose range covers a pair's units whole writes its output;
+// otherwise it leaves a partial result -- at most two, at the ends of its
+// range -- which join_kernel adds in the order of the workgroups.  (Joining in
+// the workgroup that comes last, by a counter, was tried: the results have to
+// go past the L2s of the XCDs, and a call of few pairs and many partial
+// results leaves them to one workgroup; 1 us shorter with up to 8 of them a
+// pair, 9 to 16 us longer with 64 and more.)  Calls of short sequences
+// (Attend::whole) give every pair to one workgroup instead.
 #pragma once
 
 #include "cache_internal.h"
@@ -72,6 +77,9 @@ struct Span {
         return n > 1 ? n : 1;
     }
 };
+__device__ __forceinline__ int32_t length_of(const Attend& a, int32_t b) {
+    return b < a.batch ? a.lengths[b] : 0;
+}
 __device__ __forceinline__ Span span_of(const Attend& a, int32_t length) {
     Span s;
     s.length = length < 0 ? 0 : length < a.max_len ? length : a.max_len;
@@ -95,16 +103,23 @@ __device__ __forceinline__ int32_t wave_scan(int32_t v) {
     return scan_step<0x143, 0xC>(v);    // row_bcast 31 into rows 2 and 3
 }
 
-__device__ __forceinline__ int32_t units_of(const Attend& a, int32_t b) {
-    return b < a.batch ? span_of(a, a.lengths[b]).units() : 0;
+// Places of a pair in the row: its units, then an empty one, or as many as make
+// four, for what it costs to begin and end a pair.
+__device__ __forceinline__ int32_t pair_places(int32_t units) {
+    return units + 1 > 4 ? units + 1 : 4;
+}
+// Those of sequence b, for one head tile.
+__device__ __forceinline__ int32_t places_of(const Attend& a, int32_t b,
+                                             int32_t length) {
+    return b < a.batch ? pair_places(span_of(a, length).units()) : 0;
 }
 
-// Units of the sequences from 64 on.
-__device__ __forceinline__ int32_t units_behind(const Attend& a, int lane) {
+// Places of the sequences from 64 on.
+__device__ __forceinline__ int32_t places_behind(const Attend& a, int lane) {
     int32_t total = 0;
     for (int32_t b = 64; b < a.batch; b += 64)
-        total += __builtin_amdgcn_readlane(wave_scan(units_of(a, b + lane)),
-                                           63);
+        total += __builtin_amdgcn_readlane(
+            wave_scan(places_of(a, b + lane, length_of(a, b + lane))), 63);
     return total;
 }
 
@@ -116,14 +131,14 @@ __device__ __forceinline__ int32_t uniform_load(const int32_t* p, int64_t at) {
     return ((Constant)(uintptr_t)p)[at];
 }
 
-// The workgroups that share u units: every one of them has at least one.
+// The workgroups that share u places: every one of them has at least one.
 __device__ __forceinline__ int32_t sharing(const Attend& a, int32_t u) {
     return u < a.blocks ? u : a.blocks;
 }
 __device__ __forceinline__ int32_t range_start(int32_t i, int32_t u, int32_t n) {
     return (int32_t)((int64_t)u * i / n);
 }
-// The workgroup whose range holds unit x.
+// The workgroup whose range holds place x.
 __device__ __forceinline__ int32_t range_of(int32_t x, int32_t u, int32_t n) {
     return (int32_t)((((int64_t)x + 1) * n - 1) / u);
 }
@@ -246,6 +261,18 @@ __device__ __forceinline__ void store_out(void* out, int64_t at, int dtype,
     }
 }
 
+// Writes 4 channels of a row of the output, and its lse.
+__device__ __forceinline__ void finish(const Attend& a, int dtype, int64_t row,
+                                       int d, float m, float l, f32x4 r) {
+    const bool none = l == 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : r[e] / l;
+    store_out(a.out, row * a.c.dim + d, dtype, r);
+    if (d == 0 && a.lse)
+        a.lse[row] = none ? -INFINITY
+                          : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
 // ---- the kernel ------------------------------------------------------------
 
 // The codes of a wave's 32 tokens as they are loaded.  Keys: lane l has, of
@@ -319,30 +346,46 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
     const int dim = a.c.dim;
     const int32_t pairs = a.c.kv_heads * a.head_tiles;
 
-    // this workgroup's units and the sequence of the first
-    int32_t own = units_of(a, lane);
-    int32_t sum = wave_scan(own);
-    const int32_t total =
-        (__builtin_amdgcn_readlane(sum, 63) + units_behind(a, lane)) * pairs;
-    const int32_t sharers = sharing(a, total);
+    // this workgroup's places and the pair of the first
     const int32_t self = blockIdx.x;
-    if (self >= sharers) return;
-    int32_t unit = range_start(self, total, sharers);
-    const int32_t unit_end = range_start(self + 1, total, sharers);
-    int32_t seq = 0, before = 0;     // units before seq, in one head tile
-    for (int32_t b = 0;;) {
-        const int32_t all = __builtin_amdgcn_readlane(sum, 63);
-        if (unit < (before + all) * pairs) {
-            const uint64_t past = __ballot((before + sum) * pairs > unit);
-            const int at = __builtin_ctzll(past);
-            seq = b + at;
-            before += __builtin_amdgcn_readlane(sum - own, at);
-            break;
+    int32_t place = 0, place_end = 0, pair_start = 0, seq = 0, pair = 0;
+    // lengths of 64 sequences, from `lengths_of` on
+    int32_t lengths = 0, lengths_of = 0;
+    if (a.whole) {
+        seq = self / pairs;
+        pair = self - seq * pairs;
+        lengths = uniform_load(a.lengths, seq);
+        lengths_of = seq;
+    } else {
+        lengths = length_of(a, lane);
+        int32_t own = places_of(a, lane, lengths);
+        int32_t sum = wave_scan(own);
+        const int32_t total = (__builtin_amdgcn_readlane(sum, 63) +
+                               places_behind(a, lane)) * pairs;
+        const int32_t sharers = sharing(a, total);
+        if (self >= sharers) return;
+        place = range_start(self, total, sharers);
+        place_end = range_start(self + 1, total, sharers);
+        int32_t before = 0;          // places before seq, for one head tile
+        for (int32_t b = 0;;) {
+            const int32_t all = __builtin_amdgcn_readlane(sum, 63);
+            if (place < (before + all) * pairs) {
+                const uint64_t past = __ballot((before + sum) * pairs > place);
+                const int at = __builtin_ctzll(past);
+                const int32_t its = __builtin_amdgcn_readlane(own, at);
+                seq = b + at;
+                before += __builtin_amdgcn_readlane(sum, at) - its;
+                pair = (place - before * pairs) / its;
+                pair_start = before * pairs + pair * its;
+                break;
+            }
+            before += all;
+            b += 64;
+            lengths_of = b;
+            lengths = length_of(a, b + lane);
+            own = places_of(a, b + lane, lengths);
+            sum = wave_scan(own);
         }
-        before += all;
-        b += 64;
-        own = units_of(a, b + lane);
-        sum = wave_scan(own);
     }
 
     // lane offsets, in bytes, of the codes within 16 rows; lanes behind the
@@ -357,16 +400,36 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
     const uint32_t v_at =
         4 * group * v_row + (head * kOwn < dim ? head * kOwn * VB / 8 : 0);
 
-    while (unit < unit_end) {
-        const Span span = span_of(a, uniform_load(a.lengths, seq));
+    for (bool again = false;;) {
+        if (seq - lengths_of >= 64) {
+            lengths_of = seq;
+            lengths = length_of(a, seq + lane);
+        }
+        const Span span = span_of(
+            a, __builtin_amdgcn_readlane(lengths, seq - lengths_of));
         const int32_t units = span.units();
-        const int32_t rel = unit - before * pairs;
-        const int32_t pair = rel / units;
-        const int32_t c0 = rel - pair * units;
-        const int32_t c1 =
-            units - c0 < unit_end - unit ? units : c0 + unit_end - unit;
+        // units [c0, c1) of this pair
+        int32_t c0 = 0, c1 = units;
+        if (!a.whole) {
+            c0 = min(place - pair_start, units);
+            c1 = min(place_end - pair_start, units);
+            pair_start += pair_places(units);
+            place = pair_start;
+        }
         const int32_t kvh = pair / a.head_tiles;
         const int32_t tile16 = pair - kvh * a.head_tiles;
+        const int32_t now_seq = seq;
+        if (++pair == pairs) {
+            pair = 0;
+            ++seq;
+        }
+        const bool last = a.whole || place >= place_end;
+        if (c0 >= c1) {              // nothing but empty places
+            if (last) break;
+            continue;
+        }
+        if (again) __syncthreads();  // the results of the pair before are read
+        again = true;
         const int32_t h0 = kvh * a.group + tile16 * 16;
         const int32_t heads =
             a.group - tile16 * 16 < 16 ? a.group - tile16 * 16 : 16;
@@ -374,7 +437,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
         // ---- tiles and their loads
         C codes;
         uint32_t ks[2][4], vs[2][4];
-        const int64_t table = (int64_t)seq * a.max_pages;
+        const int64_t table = (int64_t)now_seq * a.max_pages;
         auto find = [&](int32_t c) {
             Tile t;
             t.token = span.start() + c * kUnit + wave * 32;
@@ -434,7 +497,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
         const bool mine = head < heads;
         {
             const int64_t base =
-                seq * a.q_stride + (int64_t)(h0 + (mine ? head : 0)) * dim;
+                now_seq * a.q_stride + (int64_t)(h0 + (mine ? head : 0)) * dim;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 const int chunk = group + 4 * (i >> 1);
@@ -642,6 +705,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
             }
         __syncthreads();
         const bool is_whole = c0 == 0 && c1 == units;
+        const int64_t row0 = (int64_t)now_seq * a.heads + h0;
         float* part = is_whole ? nullptr
                                : part_of(a, 2 * self + (c0 > 0 ? 0 : 1));
         const int quads = dim >> 2;
@@ -662,106 +726,16 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
                 for (int e = 0; e < 4; ++e) r[e] = __builtin_fmaf(f, y[e], r[e]);
             }
             if (is_whole) {
-                const int64_t row = (int64_t)seq * a.heads + h0 + h;
-                const bool none = l == 0.0f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : r[e] / l;
-                store_out(a.out, row * dim + d, T, r);
-                if (d == 0 && a.lse)
-                    a.lse[row] = none ? -INFINITY
-                                      : (m + __builtin_amdgcn_logf(l)) * kLn2;
+                finish(a, T, row0 + h, d, m, l, r);
             } else {
                 *reinterpret_cast<f32x4*>(part + h * dim + d) = r;
-                if (d == 0) {
-                    part[16 * dim + 2 * h] = m;
-                    part[16 * dim + 2 * h + 1] = l;
-                }
+                if (d == 0)
+                    *reinterpret_cast<float2*>(part + 16 * dim + 2 * h) =
+                        make_float2(m, l);
             }
         }
-        unit += c1 - c0;
-        if (c1 == units && pair + 1 == pairs) {
-            before += units;
-            ++seq;
-        }
-        if (unit < unit_end) __syncthreads();
+        if (last) break;
     }
-}
-
-// Joins the partial results of a (sequence, query head) that several
-// workgroups share, in the order of the workgroups.
-template <int UNUSED = 0>
-__global__ __launch_bounds__(kThreads) void join_kernel(const Attend a) {
-    __shared__ f32x4 sm_o[kThreads];
-    __shared__ float sm_m[kWaves], sm_l[kThreads];
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t seq = blockIdx.x / a.heads;
-    const int32_t h = blockIdx.x - seq * a.heads;
-    const int32_t kvh = h / a.group, in_group = h - kvh * a.group;
-    const int32_t tile16 = in_group / 16, row = in_group - tile16 * 16;
-    const int32_t pairs = a.c.kv_heads * a.head_tiles;
-    const int dim = a.c.dim;
-    int32_t total = 0, before = 0;
-    for (int32_t b = 0; b < a.batch; b += 64) {
-        const int32_t own = units_of(a, b + lane);
-        const int32_t sum = wave_scan(own);
-        if (seq >= b && seq < b + 64)
-            before = total + __builtin_amdgcn_readlane(sum - own, seq - b);
-        total += __builtin_amdgcn_readlane(sum, 63);
-    }
-    total *= pairs;
-    const int32_t units = span_of(a, a.lengths[seq]).units();
-    const int32_t sharers = sharing(a, total);
-    const int32_t u0 = before * pairs + (kvh * a.head_tiles + tile16) * units;
-    const int32_t i0 = range_of(u0, total, sharers);
-    const int32_t i1 = range_of(u0 + units - 1, total, sharers);
-    if (i0 == i1) return;
-    const int32_t parts = i1 - i0 + 1;
-    auto part = [&](int32_t p) {
-        return part_of(a, 2 * (i0 + p) + (p == 0 ? 1 : 0));
-    };
-    // the largest maximum
-    float m = kNone;
-    for (int32_t p = threadIdx.x; p < parts; p += kThreads)
-        m = fmaxf(m, part(p)[16 * dim + 2 * row]);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    if (lane == 0) sm_m[wave] = m;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, sm_m[w]);
-    // columns of 4 channels, and rows of threads that take every rows-th part
-    const int quads = dim >> 2;
-    const int rows = kThreads / quads;
-    const int col = threadIdx.x % quads, mine = threadIdx.x / quads;
-    f32x4 r = {0, 0, 0, 0};
-    float l = 0.0f;
-    if (mine < rows)
-        for (int32_t p = mine; p < parts; p += rows) {
-            const float* q = part(p);
-            const float f =
-                __builtin_amdgcn_exp2f(q[16 * dim + 2 * row] - m);
-            l = __builtin_fmaf(f, q[16 * dim + 2 * row + 1], l);
-            const f32x4 y =
-                *reinterpret_cast<const f32x4*>(q + row * dim + 4 * col);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = __builtin_fmaf(f, y[e], r[e]);
-        }
-    sm_o[threadIdx.x] = r;
-    sm_l[threadIdx.x] = l;
-    __syncthreads();
-    if (mine != 0) return;
-    for (int w = 1; w < rows; ++w) {
-        r += sm_o[w * quads + col];
-        l += sm_l[w * quads + col];
-    }
-    const int64_t at = (int64_t)seq * a.heads + h;
-    const bool none = l == 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : r[e] / l;
-    store_out(a.out, at * dim + 4 * col, a.dtype, r);
-    if (col == 0 && a.lse)
-        a.lse[at] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // Launches the kernel for DP padded channels (one translation unit each).

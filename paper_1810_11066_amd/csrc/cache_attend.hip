@@ -1,29 +1,147 @@
 // Launch of the cache's attention: how many workgroups share a call, which
 // kernel takes it, and the join of their partial results.
+#include <algorithm>
+
 #include "cache_attend.h"
 
+#ifndef BS_WHOLE
+#define BS_WHOLE 4
+#endif
 namespace bscache {
+namespace {
+
+// Adds the partial results of a pair that several workgroups share, in their
+// order.  A workgroup of this kernel takes `few` query heads of one pair: all
+// of its tile where pairs are many, one where pairs are few and have many
+// partial results each.  Threads are columns of 4 channels of a head, times
+// rows that take every rows-th partial result and are added at the end; a
+// thread has kDeep of them in flight, and a running maximum of its own, so
+// that no load waits for another but the lengths'.
+constexpr int kDeep = 8;
+
+__global__ __launch_bounds__(kThreads) void join_kernel(const Attend a,
+                                                        int32_t few) {
+    __shared__ f32x4 sm_r[kThreads];
+    __shared__ float2 sm_ml[kThreads];
+    const int lane = threadIdx.x & 63;
+    const int dim = a.c.dim, quads = dim >> 2;
+    const int32_t pairs = a.c.kv_heads * a.head_tiles;
+    const int32_t slices = (min(a.group, 16) + few - 1) / few;
+    const int32_t at = blockIdx.x / slices;
+    const int32_t seq = at / pairs, pair = at - seq * pairs;
+    const int32_t kvh = pair / a.head_tiles;
+    const int32_t tile16 = pair - kvh * a.head_tiles;
+    const int32_t h0 = (blockIdx.x - at * slices) * few;
+    const int32_t heads = min(few, min(a.group - tile16 * 16, 16) - h0);
+    const int64_t row0 =
+        (int64_t)seq * a.heads + kvh * a.group + tile16 * 16 + h0;
+
+    int32_t total = 0, start = 0, length = 0;
+    for (int32_t b = 0; b < a.batch; b += 64) {
+        const int32_t its = length_of(a, b + lane);
+        const int32_t own = places_of(a, b + lane, its);
+        const int32_t sum = wave_scan(own);
+        if (seq >= b && seq < b + 64) {
+            const int32_t places = __builtin_amdgcn_readlane(own, seq - b);
+            length = __builtin_amdgcn_readlane(its, seq - b);
+            start = (total + __builtin_amdgcn_readlane(sum, seq - b) - places) *
+                        pairs + pair * places;
+        }
+        total += __builtin_amdgcn_readlane(sum, 63);
+    }
+    total *= pairs;
+    const int32_t units = span_of(a, length).units();
+    const int32_t sharers = sharing(a, total);
+    const int32_t i0 = range_of(start, total, sharers);
+    const int32_t parts =
+        range_of(start + units - 1, total, sharers) - i0 + 1;
+    if (parts == 1) return;          // its workgroup wrote the output
+
+    const int32_t columns = heads * quads;
+    const int32_t rows = columns < kThreads ? kThreads / max(columns, 1) : 1;
+    for (int32_t c0 = 0; c0 < columns; c0 += kThreads) {
+        const int32_t mine = rows > 1 ? threadIdx.x / columns : 0;
+        const int32_t column = c0 + threadIdx.x - mine * columns;
+        const int32_t h = column / quads, d = 4 * (column - h * quads);
+        const bool on = mine < rows && column < columns;
+        float m = kNone, l = 0.0f;
+        f32x4 r = {0, 0, 0, 0};
+        for (int32_t p = mine; on && p < parts; p += kDeep * rows) {
+            float2 ml[kDeep];
+            f32x4 y[kDeep];
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) {
+                const int32_t n = min(p + u * rows, parts - 1);
+                const float* q = part_of(a, 2 * (i0 + n) + (n == 0 ? 1 : 0));
+                ml[u] = *reinterpret_cast<const float2*>(q + 16 * dim +
+                                                         2 * (h0 + h));
+                y[u] = *reinterpret_cast<const f32x4*>(q + (h0 + h) * dim + d);
+                if (p + u * rows >= parts) ml[u].x = -INFINITY;  // not again
+            }
+            float top = m;
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) top = fmaxf(top, ml[u].x);
+            const float f = __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= f;
+            r *= f;
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) {
+                const float g = __builtin_amdgcn_exp2f(ml[u].x - top);
+                l = __builtin_fmaf(g, ml[u].y, l);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    r[e] = __builtin_fmaf(g, y[u][e], r[e]);
+            }
+        }
+        if (rows > 1) {              // (then there is one pass over columns)
+            sm_r[threadIdx.x] = r;
+            sm_ml[threadIdx.x] = make_float2(m, l);
+            __syncthreads();
+            if (mine == 0) {
+                for (int32_t w = 1; w < rows; ++w)
+                    m = fmaxf(m, sm_ml[w * columns + column].x);
+                l = 0.0f;
+                r = f32x4{0, 0, 0, 0};
+                for (int32_t w = 0; w < rows; ++w) {
+                    const float2 ml = sm_ml[w * columns + column];
+                    const float f = __builtin_amdgcn_exp2f(ml.x - m);
+                    l = __builtin_fmaf(f, ml.y, l);
+                    r += f * sm_r[w * columns + column];
+                }
+            }
+        }
+        if (on && mine == 0) finish(a, a.dtype, row0 + h, d, m, l, r);
+    }
+}
+
+}  // namespace
 
 template <> hipError_t launch_attend_dp<64>(const Attend&, hipStream_t);
 template <> hipError_t launch_attend_dp<128>(const Attend&, hipStream_t);
 template <> hipError_t launch_attend_dp<256>(const Attend&, hipStream_t);
 
-int attend_blocks(const Attend& a, int64_t max_units) {
-    // as many workgroups as run at once
+void plan_attend(Attend& a, int64_t units) {
+    const int64_t pairs =
+        (int64_t)a.batch * a.c.kv_heads * a.head_tiles;
     const int dp = a.c.dim > 128 ? 256 : a.c.dim > 64 ? 128 : 64;
-    const int64_t most =
-        (int64_t)device_cus() * attend_waves(dp, a.dtype);
-    const int64_t n = max_units < most ? max_units : most;
-    return (int)(n < 1 ? 1 : n);
+    // as many workgroups as run at once
+    const int64_t most = (int64_t)device_cus() * attend_waves(dp, a.dtype);
+    a.whole = units <= BS_WHOLE || (units <= 16 && 2 * pairs >= most);
+    const int64_t n = a.whole ? pairs : std::min(pairs * units, most);
+    a.blocks = (int32_t)std::max(n, (int64_t)1);
 }
 
-hipError_t launch_attend(const Attend& a, bool join, hipStream_t st) {
+hipError_t launch_attend(const Attend& a, hipStream_t st) {
     const hipError_t e = a.c.dim > 128  ? launch_attend_dp<256>(a, st)
                          : a.c.dim > 64 ? launch_attend_dp<128>(a, st)
                                         : launch_attend_dp<64>(a, st);
-    if (e != hipSuccess || !join) return e;
-    hipLaunchKernelGGL((join_kernel<0>), dim3(a.heads * a.batch),
-                       dim3(kThreads), 0, st, a);
+    if (e != hipSuccess || a.whole) return e;
+    const int32_t pairs = a.batch * a.c.kv_heads * a.head_tiles;
+    const int32_t heads = std::min(a.group, 16);
+    const int32_t few = pairs < device_cus() ? 1 : heads;
+    hipLaunchKernelGGL(join_kernel, dim3(pairs * ((heads + few - 1) / few)),
+                       dim3(kThreads), 0, st, a, few);
     return hipGetLastError();
 }
 

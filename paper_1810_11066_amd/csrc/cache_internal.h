@@ -126,7 +126,8 @@ struct Attend {
     int32_t head_tiles;       // tiles of up to 16 query heads of a kv head
     int32_t max_pages, max_len, window, dtype;
     float scale2;             // scale log2(e)
-    int32_t blocks;           // workgroups that share the units
+    bool whole;               // every pair is one workgroup's
+    int32_t blocks;           // workgroups
 };
 
 // Waves of a SIMD that the attention kernel for dp padded channels and a type
@@ -138,9 +139,10 @@ constexpr int attend_waves(int dp, int dtype) {
 // Tokens of a unit: what the waves of a workgroup take in one step.
 constexpr int kUnit = 128;
 
-// Workgroups for a call, and whether several may share a sequence's head tile.
-int attend_blocks(const Attend& a, int64_t max_units);
+// Chooses `whole` and `blocks` for a call whose longest sequence has `units`
+// units.
+void plan_attend(Attend& a, int64_t units);
 
-hipError_t launch_attend(const Attend& a, bool join, hipStream_t st);
+hipError_t launch_attend(const Attend& a, hipStream_t st);
 
 }  // namespace bscache
