@@ -26,9 +26,9 @@ constexpr int kBlock = 256;
 // order in it, and one LDS permutation for 32.
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
-    const int i = __builtin_bit_cast(int, v);
     return __builtin_bit_cast(
-        float, __builtin_amdgcn_update_dpp(i, i, CTRL, 0xF, 0xF, false));
+        float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL,
+                                           0xF, 0xF, true));
 }
 template <int LPR, class F>
 __device__ __forceinline__ float reduce_row(float v, F f) {
@@ -40,10 +40,18 @@ __device__ __forceinline__ float reduce_row(float v, F f) {
     return v;
 }
 
-// x as the quantizer takes it.
+// x as the quantizer takes it: 0 for NaN, within +-kBig.  The smaller and the
+// larger of two such values as medians with a bound (v_med3_f32; fminf and
+// fmaxf take an instruction more each, which quiets NaNs that are not there).
+constexpr float kBig = 0x1p126f;
 __device__ __forceinline__ float finite(float x) {
-    const float r = __builtin_amdgcn_fmed3f(x, -0x1p126f, 0x1p126f);
-    return x == x ? r : 0.0f;
+    return __builtin_amdgcn_fmed3f(x == x ? x : 0.0f, -kBig, kBig);
+}
+__device__ __forceinline__ float smaller(float a, float b) {
+    return __builtin_amdgcn_fmed3f(a, b, -kBig);
+}
+__device__ __forceinline__ float larger(float a, float b) {
+    return __builtin_amdgcn_fmed3f(a, b, kBig);
 }
 
 // Which rows a wave has: all tokens of a stretch for one (head, side).
@@ -69,14 +77,16 @@ __device__ __forceinline__ bool wave_rows(const RowsGrid& g, int per,
     return true;
 }
 
-// Codes of 8 values in 8 or 4 bits: fl32((x - z) * inv) rounded half to even
-// and clamped, by the library's quantizer.
+// Codes of 8 values: fl32(fl32(x - z) * inv) rounded half to even, as bytes
+// (v_cvt_pk_u8_f32).  The clamp of the definition never binds: x >= z, and
+// (x - z) inv <= (2^B - 1) (1 + 2^-21), which rounds to 2^B - 1.
 __device__ __forceinline__ u32x2 codes8(const float (&x)[8], float z,
-                                        float inv, float top) {
+                                        float inv) {
     u32x2 d = {0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        d[i >> 2] = bs::quant_insert(x[i] - z, inv, top, i & 3, d[i >> 2]);
+        d[i >> 2] = __builtin_amdgcn_cvt_pk_u8_f32((x[i] - z) * inv, i & 3,
+                                                   d[i >> 2]);
     return d;
 }
 // the low halves of 4 bytes as 2 bytes
@@ -85,12 +95,30 @@ __device__ __forceinline__ uint32_t nibbles(uint32_t d) {
     return (d | d >> 8) & 0xFFFFu;
 }
 
+// the four nibbles of 2 bytes as 4 bytes
+__device__ __forceinline__ uint32_t spread(uint32_t w) {
+    w = (w | w << 8) & 0x00FF00FFu;
+    return (w | w << 4) & 0x0F0F0F0Fu;
+}
+
+// A large call's results go past the caches (non-temporal stores): they push
+// out nothing that is read sooner, and are not fetched before they are
+// written.
+template <bool STREAM, class V>
+__device__ __forceinline__ void put(V* p, V v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
+// Bound by memory, and next by the vector ALUs (about 130 instructions for 8
+// channels a lane: 16 bytes of float16).
 template <int T, int LPR, int STEPS>
 __global__ __launch_bounds__(kBlock) void write_kernel(
     Pages c, const void* __restrict__ k, const void* __restrict__ v,
     int64_t k_stride, int64_t v_stride, const int32_t* __restrict__ slots,
     RowsGrid g) {
     constexpr int kRows = 64 / LPR;
+    constexpr bool kStream = STEPS > 1;
     int side, head;
     int64_t first;
     if (!wave_rows(g, kRows * STEPS, side, head, first)) return;
@@ -100,31 +128,32 @@ __global__ __launch_bounds__(kBlock) void write_kernel(
     const void* src = side ? v : k;
     const int64_t stride = side ? v_stride : k_stride;
     const int bits = c.bits[side];
-    const float top = bits == 8 ? 255.0f : 15.0f;
     const float per = bits == 8 ? 1.0f / 255.0f : 1.0f / 15.0f;
     uint32_t slot[STEPS];
     Eight<T> in[STEPS];
+    const int64_t t0 = first + lane / LPR;
+    int64_t at = t0 * stride + (int64_t)head * c.dim + channel;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        const int64_t t = first + s * kRows + lane / LPR;
+    for (int s = 0; s < STEPS; ++s, at += kRows * stride) {
+        const int64_t t = t0 + s * kRows;
         slot[s] = t < g.tokens ? (uint32_t)slots[t] : ~0u;
-        if (t < g.tokens && mine)
-            in[s].load(src, t * stride + (int64_t)head * c.dim + channel);
-        else
-            in[s].clear();
+        if (t < g.tokens && mine) in[s].load(src, at);
+        else in[s].clear();
     }
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        float x[8], lo = INFINITY, hi = -INFINITY;
+        float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = finite(in[s].get(i));
-            lo = fminf(lo, x[i]);
-            hi = fmaxf(hi, x[i]);
+        for (int i = 0; i < 8; ++i) x[i] = finite(in[s].get(i));
+        float lo = x[0], hi = x[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+            lo = smaller(lo, x[i]);
+            hi = larger(hi, x[i]);
         }
-        if (!mine) lo = INFINITY, hi = -INFINITY;
-        lo = reduce_row<LPR>(lo, [](float a, float b) { return fminf(a, b); });
-        hi = reduce_row<LPR>(hi, [](float a, float b) { return fmaxf(a, b); });
+        if (!mine) lo = kBig, hi = -kBig;
+        lo = reduce_row<LPR>(lo, smaller);
+        hi = reduce_row<LPR>(hi, larger);
         // z down to bfloat16 (towards zero by dropping the low half, one
         // step on where that went up), s up
         const uint32_t lb = f32_bits(lo), lcut = lb & 0xFFFF0000u;
@@ -138,64 +167,76 @@ __global__ __launch_bounds__(kBlock) void write_kernel(
             const uint32_t page = c.by_page.div(slot[s]);
             const int64_t row =
                 row_of(c, page, head, slot[s] - page * c.by_page.d);
-            const u32x2 d = codes8(x, z, inv, top);
+            const u32x2 d = codes8(x, z, inv);
             uint8_t* codes = c.codes[side];
             if (bits == 8)
-                *reinterpret_cast<u32x2*>(codes + row * c.dim + channel) = d;
+                put<kStream>(reinterpret_cast<u32x2*>(codes + row * c.dim +
+                                                      channel), d);
             else
-                *reinterpret_cast<uint32_t*>(codes + row * (c.dim >> 1) +
-                                             (channel >> 1)) =
-                    nibbles(d[0]) | nibbles(d[1]) << 16;
+                put<kStream>(reinterpret_cast<uint32_t*>(
+                                 codes + row * (c.dim >> 1) + (channel >> 1)),
+                             nibbles(d[0]) | nibbles(d[1]) << 16);
             if (part == 0) c.steps[side][row] = f32_bits(step) >> 16 | zb;
         }
     }
 }
 
+// A lane's codes are two times 4 channels: next to each other where the values
+// are written as one 16-byte store of 16 bits each, LPR lanes apart where they
+// are float32, so that a store of 4 of them leaves no gap between the lanes.
 template <int T, int LPR, int STEPS>
 __global__ __launch_bounds__(kBlock) void read_kernel(
     Pages c, const int32_t* __restrict__ slots, void* __restrict__ k,
     void* __restrict__ v, RowsGrid g) {
     constexpr int kRows = 64 / LPR;
+    constexpr int kApart = T == kF32 ? 4 * LPR : 4;
     int side, head;
     int64_t first;
     if (!wave_rows(g, kRows * STEPS, side, head, first)) return;
     const int lane = threadIdx.x & 63;
-    const int channel = lane % LPR * 8;
-    const bool mine = channel < c.dim;
+    const int channel = lane % LPR * (T == kF32 ? 4 : 8);
     const int bits = c.bits[side];
     const uint8_t* codes = c.codes[side];
-    u32x2 d[STEPS];
-    uint32_t sz[STEPS];
+    uint32_t d[STEPS][2], sz[STEPS];
+    const int64_t t0 = first + lane / LPR;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        const int64_t t = first + s * kRows + lane / LPR;
+        const int64_t t = t0 + s * kRows;
         const uint32_t slot = t < g.tokens ? (uint32_t)slots[t] : ~0u;
-        d[s] = u32x2{0, 0};
-        sz[s] = 0;            // a slot outside the cache: 0 + 0 c
-        if (slot < c.slots && mine) {
+        d[s][0] = d[s][1] = sz[s] = 0;     // a slot outside the cache: 0 + 0 c
+        if (slot < c.slots && channel < c.dim) {
             const uint32_t page = c.by_page.div(slot);
             const int64_t row = row_of(c, page, head,
                                        slot - page * c.by_page.d);
             sz[s] = c.steps[side][row];
-            if (bits == 8) {
-                d[s] = *reinterpret_cast<const u32x2*>(codes + row * c.dim +
-                                                       channel);
+            const uint8_t* p = codes + row * (c.dim * bits >> 3) +
+                               (channel * bits >> 3);
+            if constexpr (T == kF32) {
+                const bool both = channel + kApart < c.dim;
+                if (bits == 8) {
+                    d[s][0] = *reinterpret_cast<const uint32_t*>(p);
+                    if (both)
+                        d[s][1] = *reinterpret_cast<const uint32_t*>(p + kApart);
+                } else {
+                    d[s][0] = spread(*reinterpret_cast<const uint16_t*>(p));
+                    if (both)
+                        d[s][1] = spread(
+                            *reinterpret_cast<const uint16_t*>(p + kApart / 2));
+                }
+            } else if (bits == 8) {
+                const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+                d[s][0] = w[0], d[s][1] = w[1];
             } else {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(
-                    codes + row * (c.dim >> 1) + (channel >> 1));
-                // bytes of codes 0, 2, 4, 6 and 1, 3, 5, 7, interleaved
-                const uint32_t even = w & 0x0F0F0F0Fu,
-                               odd = w >> 4 & 0x0F0F0F0Fu;
-                d[s][0] = __builtin_amdgcn_perm(odd, even, 0x05010400u);
-                d[s][1] = __builtin_amdgcn_perm(odd, even, 0x07030602u);
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+                d[s][0] = spread(w & 0xFFFFu), d[s][1] = spread(w >> 16);
             }
         }
     }
     void* dst = side ? v : k;
+    int64_t at = (t0 * c.kv_heads + head) * c.dim + channel;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        const int64_t t = first + s * kRows + lane / LPR;
-        if (t >= g.tokens || !mine) continue;
+    for (int s = 0; s < STEPS; ++s, at += (int64_t)kRows * c.kv_heads * c.dim) {
+        if (t0 + s * kRows >= g.tokens || channel >= c.dim) continue;
         const float step = step_of(sz[s]), z = offset_of(sz[s]);
         float x[8];
 #pragma unroll
@@ -203,16 +244,19 @@ __global__ __launch_bounds__(kBlock) void read_kernel(
             const float code = (float)(d[s][i >> 2] >> 8 * (i & 3) & 255u);
             x[i] = z + code * step;      // the product is exact
         }
-        const int64_t at = (t * c.kv_heads + head) * c.dim + channel;
         if constexpr (T == kF32) {
-            f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(dst) + at);
-            p[0] = f32x4{x[0], x[1], x[2], x[3]};
-            p[1] = f32x4{x[4], x[5], x[6], x[7]};
+            float* p = static_cast<float*>(dst) + at;
+            put<true>(reinterpret_cast<f32x4*>(p),
+                      f32x4{x[0], x[1], x[2], x[3]});
+            if (channel + kApart < c.dim)
+                put<true>(reinterpret_cast<f32x4*>(p + kApart),
+                          f32x4{x[4], x[5], x[6], x[7]});
         } else {
             u32x4 w;
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
-            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dst) + at) = w;
+            put<true>(reinterpret_cast<u32x4*>(static_cast<uint16_t*>(dst) +
+                                               at), w);
         }
     }
 }
