@@ -27,8 +27,8 @@ constexpr int kBlock = 256;
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
     return __builtin_bit_cast(
-        float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL,
-                                           0xF, 0xF, true));
+        float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF,
+                                        0xF, true));
 }
 template <int LPR, class F>
 __device__ __forceinline__ float reduce_row(float v, F f) {
@@ -41,8 +41,9 @@ __device__ __forceinline__ float reduce_row(float v, F f) {
 }
 
 // x as the quantizer takes it: 0 for NaN, within +-kBig.  The smaller and the
-// larger of two such values as medians with a bound (v_med3_f32; fminf and
-// fmaxf take an instruction more each, which quiets NaNs that are not there).
+// larger of two such values as medians with a bound (v_med3_f32): after a DPP
+// move fminf and fmaxf take an instruction more each, which quiets NaNs that
+// are not there.
 constexpr float kBig = 0x1p126f;
 __device__ __forceinline__ float finite(float x) {
     return __builtin_amdgcn_fmed3f(x == x ? x : 0.0f, -kBig, kBig);
@@ -148,8 +149,8 @@ __global__ __launch_bounds__(kBlock) void write_kernel(
         float lo = x[0], hi = x[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) {
-            lo = smaller(lo, x[i]);
-            hi = larger(hi, x[i]);
+            lo = fminf(lo, x[i]);
+            hi = fmaxf(hi, x[i]);
         }
         if (!mine) lo = kBig, hi = -kBig;
         lo = reduce_row<LPR>(lo, smaller);
