@@ -19,6 +19,7 @@ page * page_tokens + its place in the page.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import struct
 import threading
@@ -40,9 +41,8 @@ EXPORTED = ("bscache_write", "bscache_read", "bscache_attend",
             "bscache_attend_workspace", "bscache_last_error",
             "bscache_abi_version")
 
-# bscache_dtype and bytes of an element
-_DTYPES = {torch.float32: (0, 4), torch.float16: (1, 2),
-           torch.bfloat16: (2, 2)}
+# bscache_dtype
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 class CacheError(RuntimeError):
@@ -119,22 +119,22 @@ def _stream(device: int) -> int:
     return _raw_stream(device)
 
 
-def _on(device: int, call, *args) -> None:
-    """The call with the tensors' device as the current one."""
+def _call(device: int, fn, *args) -> None:
+    """The C call with the tensors' device as the current one."""
     current = torch.cuda.current_device() if _raw_device is None \
         else _raw_device()
     if current == device:
-        _check(call(*args))
+        status = fn(*args)
     else:
         with torch.cuda.device(device):
-            _check(call(*args))
+            status = fn(*args)
+    if status != OK:
+        _check(status)
 
 
-def _plain(t, name: str, dtype, dims: int, device: int) -> None:
-    """A contiguous GPU tensor of the given type and rank on `device`."""
-    if (isinstance(t, torch.Tensor) and t.dtype == dtype and t.dim() == dims
-            and t.is_cuda and t.get_device() == device and t.is_contiguous()):
-        return
+def _refuse(t, name: str, dtype, dims: int, device: int):
+    """Raises what is wrong with a tensor that should be a contiguous one of
+    the given type and rank on `device`."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
     if not t.is_cuda:
@@ -147,7 +147,17 @@ def _plain(t, name: str, dtype, dims: int, device: int) -> None:
     if t.dim() != dims:
         raise ValueError("%s must have %d axes (got %s)"
                          % (name, dims, tuple(t.shape)))
-    raise ValueError("%s must be contiguous" % name)
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+
+
+def _int32(t, name: str, dims: int, device: int):
+    """Shape of a contiguous int32 tensor on `device`."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32
+            and t.get_device() == device and t.is_contiguous()
+            and t.dim() == dims):
+        _refuse(t, name, torch.int32, dims, device)
+    return t.shape
 
 
 def _rows(t, name: str, heads: int, dim: int, device: int):
@@ -159,7 +169,7 @@ def _rows(t, name: str, heads: int, dim: int, device: int):
     if kind is None:
         raise TypeError("%s must be float32, float16 or bfloat16 (got %s)"
                         % (name, t.dtype))
-    if not t.is_cuda or t.get_device() != device:
+    if t.get_device() != device:
         raise ValueError("%s is on %s, the cache on cuda:%d"
                          % (name, t.device, device))
     shape = t.shape
@@ -171,36 +181,66 @@ def _rows(t, name: str, heads: int, dim: int, device: int):
         raise ValueError("%s: a token's heads and channels must lie together "
                          "(strides %s)" % (name, (s0, s1, s2)))
     # a lone token has no distance to a next one
-    return kind[0], s0 if shape[0] > 1 else heads * dim
+    return kind, s0 if shape[0] > 1 else heads * dim
 
 
 def _pages(cache, dim: int):
     """(packed bscache_pages, kv_heads, page_tokens, device) of a cache whose
     rows have `dim` channels."""
+    kc, ks, vc, vs = cache
+    # all of it at once; what is wrong is looked for only if something is
+    try:
+        device = kc.get_device()
+        pages, heads, tokens, k_row = shape = kc.shape
+        v_row = vc.shape[3]
+        good = (device >= 0 and kc.dtype is torch.uint8
+                and vc.dtype is torch.uint8 and ks.dtype is torch.bfloat16
+                and vs.dtype is torch.bfloat16 and ks.get_device() == device
+                and vc.get_device() == device and vs.get_device() == device
+                and kc.is_contiguous() and ks.is_contiguous()
+                and vc.is_contiguous() and vs.is_contiguous()
+                and ks.shape == (pages, heads, tokens, 2) == vs.shape
+                and (k_row == v_row and vc.shape == shape
+                     or vc.shape == (pages, heads, tokens, v_row))
+                and dim >= 1 and k_row * 8 % dim == 0 == v_row * 8 % dim)
+    except (AttributeError, IndexError, ValueError):
+        good = False
+    if not good:
+        _refuse_cache(cache, dim)
+    return _PAGES.pack(pages, heads, tokens, dim, k_row * 8 // dim,
+                       v_row * 8 // dim, kc.data_ptr(), ks.data_ptr(),
+                       vc.data_ptr(), vs.data_ptr()), heads, tokens, device
+
+
+def _refuse_cache(cache, dim: int):
+    """Raises what is wrong with a cache."""
+    device = cache[0].get_device() if isinstance(cache[0], torch.Tensor) else 0
+    for t, name, dtype in zip(cache, Pages._fields,
+                              (torch.uint8, torch.bfloat16) * 2):
+        _refuse(t, name, dtype, 4, device)
     k_codes, k_steps, v_codes, v_steps = cache
-    if not isinstance(k_codes, torch.Tensor):
-        raise TypeError("k_codes must be a torch.Tensor")
-    if not k_codes.is_cuda:
-        raise ValueError("k_codes must be a GPU tensor")
-    device = k_codes.get_device()
-    _plain(k_codes, "k_codes", torch.uint8, 4, device)
-    _plain(k_steps, "k_steps", torch.bfloat16, 4, device)
-    _plain(v_codes, "v_codes", torch.uint8, 4, device)
-    _plain(v_steps, "v_steps", torch.bfloat16, 4, device)
-    pages, heads, tokens, k_row = k_codes.shape
-    v_row = v_codes.shape[3]
     if (v_codes.shape[:3] != k_codes.shape[:3]
-            or k_steps.shape != (pages, heads, tokens, 2)
+            or k_steps.shape != k_codes.shape[:3] + (2,)
             or v_steps.shape != k_steps.shape):
         raise ValueError("the cache's tensors differ in pages, heads or "
                          "tokens: %s" % [tuple(t.shape) for t in cache])
-    if dim < 1 or k_row * 8 % dim or v_row * 8 % dim:
-        raise ValueError("codes of %d and %d bytes do not hold rows of %d "
-                         "channels" % (k_row, v_row, dim))
-    return _PAGES.pack(pages, heads, tokens, dim, k_row * 8 // dim,
-                       v_row * 8 // dim, k_codes.data_ptr(),
-                       k_steps.data_ptr(), v_codes.data_ptr(),
-                       v_steps.data_ptr()), heads, tokens, device
+    raise ValueError("codes of %d and %d bytes do not hold rows of %d channels"
+                     % (k_codes.shape[3], v_codes.shape[3], dim))
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace(device: int, pages: int, kv_heads: int, page_tokens: int,
+               dim: int, batch: int, heads: int, max_pages: int, max_len: int,
+               window: int, dtype: int) -> int:
+    """Bytes that bscache_attend_workspace asks for: of the sizes alone, and
+    the device's compute units."""
+    need = ctypes.c_int64()
+    cache = _PAGES.pack(pages, kv_heads, page_tokens, dim, 8, 8, 0, 0, 0, 0)
+    params = _PARAMS.pack(heads * dim, batch, heads, max_pages, max_len,
+                          window, dtype, 1.0)
+    _call(device, load_library().bscache_attend_workspace, cache, params,
+          ctypes.byref(need))
+    return need.value
 
 
 # ---- the operators ----------------------------------------------------------
@@ -235,8 +275,7 @@ def write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache,
     pages, heads, _, device = _pages(cache, dim)
     kind, k_stride = _rows(k, "k", heads, dim, device)
     v_kind, v_stride = _rows(v, "v", heads, dim, device)
-    _plain(slots, "slots", torch.int32, 1, device)
-    tokens = slots.shape[0]
+    tokens, = _int32(slots, "slots", 1, device)
     if v_kind != kind:
         raise TypeError("k is %s, v %s" % (k.dtype, v.dtype))
     if k.shape[0] != tokens or v.shape[0] != tokens:
@@ -244,9 +283,9 @@ def write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache,
                          % (k.shape[0], v.shape[0], tokens))
     if tokens == 0:
         return
-    _on(device, load_library().bscache_write, pages, k.data_ptr(),
-        v.data_ptr(), k_stride, v_stride, kind, slots.data_ptr(), tokens,
-        _stream(device))
+    _call(device, (_lib or load_library()).bscache_write, pages, k.data_ptr(),
+          v.data_ptr(), k_stride, v_stride, kind, slots.data_ptr(), tokens,
+          _stream(device))
 
 
 def read(slots: torch.Tensor, cache, dim: int, dtype=torch.float32,
@@ -263,13 +302,13 @@ def read(slots: torch.Tensor, cache, dim: int, dtype=torch.float32,
         raise TypeError("dtype must be float32, float16 or bfloat16 (got %s)"
                         % (dtype,))
     pages, heads, _, device = _pages(cache, dim)
-    _plain(slots, "slots", torch.int32, 1, device)
-    tokens = slots.shape[0]
+    tokens, = _int32(slots, "slots", 1, device)
     k = torch.empty((tokens, heads, dim), dtype=dtype, device=slots.device)
     v = torch.empty_like(k)
     if tokens:
-        _on(device, load_library().bscache_read, pages, slots.data_ptr(),
-            tokens, k.data_ptr(), v.data_ptr(), kind[0], _stream(device))
+        _call(device, (_lib or load_library()).bscache_read, pages,
+              slots.data_ptr(), tokens, k.data_ptr(), v.data_ptr(), kind,
+              _stream(device))
     return k, v
 
 
@@ -295,28 +334,24 @@ def attend(q: torch.Tensor, cache, table: torch.Tensor, lengths: torch.Tensor,
     batch, heads, dim = q.shape
     pages, kv_heads, page_tokens, device = _pages(cache, dim)
     kind, q_stride = _rows(q, "q", heads, dim, device)
-    _plain(table, "table", torch.int32, 2, device)
-    _plain(lengths, "lengths", torch.int32, 1, device)
-    if table.shape[0] != batch or lengths.shape[0] != batch:
+    rows, max_pages = _int32(table, "table", 2, device)
+    if rows != batch or _int32(lengths, "lengths", 1, device)[0] != batch:
         raise ValueError("%d queries, %d rows of the table and %d lengths"
-                         % (batch, table.shape[0], lengths.shape[0]))
-    max_pages = table.shape[1]
+                         % (batch, rows, lengths.shape[0]))
     if max_len is None:
         max_len = max_pages * page_tokens
-    params = _PARAMS.pack(q_stride, batch, heads, max_pages, max_len, window,
-                          kind, dim ** -0.5 if scale is None else scale)
-    out = torch.empty((batch, heads, dim), dtype=q.dtype, device=q.device)
+    need = _workspace(device, cache[0].shape[0], kv_heads, page_tokens, dim,
+                      batch, heads, max_pages, max_len, window, kind)
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
     lse = torch.empty((batch, heads), dtype=torch.float32, device=q.device)
-    lib = load_library()
-    need = ctypes.c_int64()
-    _on(device, lib.bscache_attend_workspace, pages, params,
-        ctypes.byref(need))
     if batch == 0:
         return out, lse
-    need = need.value
     space = torch.empty(need, dtype=torch.uint8, device=q.device) if need \
         else None
-    _on(device, lib.bscache_attend, pages, params, q.data_ptr(),
-        table.data_ptr(), lengths.data_ptr(), out.data_ptr(), lse.data_ptr(),
-        space.data_ptr() if need else None, need, _stream(device))
+    _call(device, (_lib or load_library()).bscache_attend, pages,
+          _PARAMS.pack(q_stride, batch, heads, max_pages, max_len, window,
+                       kind, dim ** -0.5 if scale is None else scale),
+          q.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(),
+          lse.data_ptr(), space.data_ptr() if need else None, need,
+          _stream(device))
     return out, lse

@@ -317,6 +317,14 @@ __device__ __forceinline__ void load_words(Rsrc rows, uint32_t at,
     }
 }
 
+// x, as a value that the compiler computes with from here on only: what is
+// derived from it is not computed ahead of the loops, where it would take
+// registers from them (11 to 54 spilled, in the loops too).
+__device__ __forceinline__ int here(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // Where the two halves of a wave's tile lie: the row of each half's first
 // token, and the end of its visible tokens (0 where its page is none of the
 // cache).  Half a tile never leaves a page (pages are multiples of 16 tokens).
@@ -342,7 +350,6 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int head = lane & 15, group = lane >> 4;
     const int dim = a.c.dim;
     const int32_t pairs = a.c.kv_heads * a.head_tiles;
 
@@ -388,18 +395,6 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
         }
     }
 
-    // lane offsets, in bytes, of the codes within 16 rows; lanes behind the
-    // last channel read their row's first codes (their products are dropped)
-    const int k_row = dim * KB / 8, v_row = dim * VB / 8;
-    uint32_t k_at[C::kChunks];
-#pragma unroll
-    for (int j = 0; j < C::kChunks; ++j) {
-        const int chunk = group + 4 * j;
-        k_at[j] = head * k_row + (chunk * 16 < dim ? chunk * 2 * KB : 0);
-    }
-    const uint32_t v_at =
-        4 * group * v_row + (head * kOwn < dim ? head * kOwn * VB / 8 : 0);
-
     for (bool again = false;;) {
         if (seq - lengths_of >= 64) {
             lengths_of = seq;
@@ -433,6 +428,20 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
         const int32_t h0 = kvh * a.group + tile16 * 16;
         const int32_t heads =
             a.group - tile16 * 16 < 16 ? a.group - tile16 * 16 : 16;
+
+        const int my_lane = here(lane);
+        const int head = my_lane & 15, group = my_lane >> 4;
+        // lane offsets, in bytes, of the codes within 16 rows; lanes behind the
+        // last channel read their row's first codes (their products are dropped)
+        const int k_row = dim * KB / 8, v_row = dim * VB / 8;
+        uint32_t k_at[C::kChunks];
+#pragma unroll
+        for (int j = 0; j < C::kChunks; ++j) {
+            const int chunk = group + 4 * j;
+            k_at[j] = head * k_row + (chunk * 16 < dim ? chunk * 2 * KB : 0);
+        }
+        const uint32_t v_at =
+            4 * group * v_row + (head * kOwn < dim ? head * kOwn * VB / 8 : 0);
 
         // ---- tiles and their loads
         C codes;
@@ -686,11 +695,13 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
         // ---- the four waves' results
         sum_p = over_groups(sum_p, add);
         sum_z = over_groups(sum_z, add);
-        if (group == 0) {
-            sm_m[wave][head] = mo;
-            sm_l[wave][head] = sum_p;
+        const int end_lane = here(lane);
+        const int col = end_lane & 15, quarter = end_lane >> 4;
+        if (quarter == 0) {
+            sm_m[wave][col] = mo;
+            sm_l[wave][col] = sum_p;
         }
-        // o[j][i] is channel kOwn (4 group + i) + j of this lane's head
+        // o[j][i] is channel kOwn (4 (lane / 16) + i) + j of head lane % 16
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -701,7 +712,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
                     r[e] = __builtin_fmaf(
                         o[j + e][i], value_factor<VB>(j + e) * kCode, sum_z);
                 *reinterpret_cast<f32x4*>(
-                    &sm_o[wave][head][kOwn * (4 * group + i) + j]) = r;
+                    &sm_o[wave][col][kOwn * (4 * quarter + i) + j]) = r;
             }
         __syncthreads();
         const bool is_whole = c0 == 0 && c1 == units;
@@ -709,7 +720,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
         float* part = is_whole ? nullptr
                                : part_of(a, 2 * self + (c0 > 0 ? 0 : 1));
         const int quads = dim >> 2;
-        for (int n = threadIdx.x; n < heads * quads; n += kThreads) {
+        for (int n = 64 * wave + end_lane; n < heads * quads; n += kThreads) {
             const int h = n / quads, d = 4 * (n - h * quads);
             float m = sm_m[0][h];
 #pragma unroll

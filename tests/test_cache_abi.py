@@ -260,9 +260,9 @@ def test_calls_run_on_the_tensors_device(monkeypatch):
     monkeypatch.setattr(kc, "_raw_device", lambda: 0)
     monkeypatch.setattr(kc, "_raw_stream", lambda d: 100 + d)
     monkeypatch.setattr(torch.cuda, "device", Guard)
-    kc._on(0, lambda: kc.OK)
+    kc._call(0, lambda: kc.OK)
     assert entered == []
-    kc._on(2, lambda: kc.OK)
+    kc._call(2, lambda: kc.OK)
     assert entered == [2, "out"]
     assert kc._stream(2) == 102
     monkeypatch.setattr(kc, "_raw_stream", None)
