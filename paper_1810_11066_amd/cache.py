@@ -303,7 +303,7 @@ def read(slots: torch.Tensor, cache, dim: int, dtype=torch.float32,
                         % (dtype,))
     pages, heads, _, device = _pages(cache, dim)
     tokens, = _int32(slots, "slots", 1, device)
-    k = torch.empty((tokens, heads, dim), dtype=dtype, device=slots.device)
+    k = torch.empty(tokens, heads, dim, dtype=dtype, device=slots.device)
     v = torch.empty_like(k)
     if tokens:
         _call(device, (_lib or load_library()).bscache_read, pages,
@@ -343,7 +343,7 @@ def attend(q: torch.Tensor, cache, table: torch.Tensor, lengths: torch.Tensor,
     need = _workspace(device, cache[0].shape[0], kv_heads, page_tokens, dim,
                       batch, heads, max_pages, max_len, window, kind)
     out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    lse = torch.empty((batch, heads), dtype=torch.float32, device=q.device)
+    lse = torch.empty(batch, heads, dtype=torch.float32, device=q.device)
     if batch == 0:
         return out, lse
     space = torch.empty(need, dtype=torch.uint8, device=q.device) if need \

@@ -286,27 +286,21 @@ hipError_t pick(int dtype, int lpr, int steps, A... a) {
     }
 }
 
-template <class... P, class... A>
-hipError_t launch(void (*fn)(P...), uint32_t blocks, hipStream_t st, A... a) {
-    hipLaunchKernelGGL(fn, dim3(blocks), dim3(kBlock), 0, st, a...);
-    return hipGetLastError();
-}
-
 template <int T, int LPR, int STEPS>
 struct Write {
     static hipError_t go(const Pages& c, const void* k, const void* v,
                          int64_t ks, int64_t vs, const int32_t* slots,
                          RowsGrid g, hipStream_t st) {
-        return launch(write_kernel<T, LPR, STEPS>, (g.waves + 3) / 4, st, c, k,
-                      v, ks, vs, slots, g);
+        return launch(write_kernel<T, LPR, STEPS>, (g.waves + 3) / 4, kBlock,
+                      st, c, k, v, ks, vs, slots, g);
     }
 };
 template <int T, int LPR, int STEPS>
 struct Read {
     static hipError_t go(const Pages& c, const int32_t* slots, void* k,
                          void* v, RowsGrid g, hipStream_t st) {
-        return launch(read_kernel<T, LPR, STEPS>, (g.waves + 3) / 4, st, c,
-                      slots, k, v, g);
+        return launch(read_kernel<T, LPR, STEPS>, (g.waves + 3) / 4, kBlock,
+                      st, c, slots, k, v, g);
     }
 };
 

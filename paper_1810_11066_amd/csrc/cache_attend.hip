@@ -4,9 +4,6 @@
 
 #include "cache_attend.h"
 
-#ifndef BS_WHOLE
-#define BS_WHOLE 4
-#endif
 namespace bscache {
 namespace {
 
@@ -121,14 +118,22 @@ template <> hipError_t launch_attend_dp<64>(const Attend&, hipStream_t);
 template <> hipError_t launch_attend_dp<128>(const Attend&, hipStream_t);
 template <> hipError_t launch_attend_dp<256>(const Attend&, hipStream_t);
 
+// A pair to one workgroup needs no plan of the lengths and no join (4.4 us and a
+// launch), but the longest sequence sets the time: about 1 us a unit and 4.5 us
+// besides.  (us a pass, pairs whole / shared: 8 pairs of 4 units 8.9 / 9.7, of 8
+// units 13.1 / 10.6; 512 pairs of 8 units 33 / 41, of 16 units 34 / 40, where
+// the GPU is full either way.)  So: up to 4 units always, up to 16 where there
+// are pairs for half of the workgroups that run at once -- there a batch with
+// one long sequence among short ones loses at most the 16 us of its units.
 void plan_attend(Attend& a, int64_t units) {
-    const int64_t pairs =
-        (int64_t)a.batch * a.c.kv_heads * a.head_tiles;
+    const int64_t pairs = (int64_t)a.batch * a.c.kv_heads * a.head_tiles;
     const int dp = a.c.dim > 128 ? 256 : a.c.dim > 64 ? 128 : 64;
-    // as many workgroups as run at once
-    const int64_t most = (int64_t)device_cus() * attend_waves(dp, a.dtype);
-    a.whole = units <= BS_WHOLE || (units <= 16 && 2 * pairs >= most);
-    const int64_t n = a.whole ? pairs : std::min(pairs * units, most);
+    const int64_t at_once = (int64_t)device_cus() * attend_waves(dp, a.dtype);
+    a.whole = units <= 4 || (units <= 16 && 2 * pairs >= at_once);
+    // shared units: as many workgroups as run at once, each with its part (4
+    // times as many, taken up as others end: 524 -> 551 us at 128 sequences of
+    // 12-16 Ki tokens)
+    const int64_t n = a.whole ? pairs : std::min(pairs * units, at_once);
     a.blocks = (int32_t)std::max(n, (int64_t)1);
 }
 
@@ -140,9 +145,8 @@ hipError_t launch_attend(const Attend& a, hipStream_t st) {
     const int32_t pairs = a.batch * a.c.kv_heads * a.head_tiles;
     const int32_t heads = std::min(a.group, 16);
     const int32_t few = pairs < device_cus() ? 1 : heads;
-    hipLaunchKernelGGL(join_kernel, dim3(pairs * ((heads + few - 1) / few)),
-                       dim3(kThreads), 0, st, a, few);
-    return hipGetLastError();
+    return launch(join_kernel, pairs * ((heads + few - 1) / few), kThreads, st,
+                  a, few);
 }
 
 }  // namespace bscache

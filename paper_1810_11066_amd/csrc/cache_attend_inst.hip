@@ -7,9 +7,7 @@ namespace {
 
 template <int DP, int KB, int VB, int T>
 hipError_t go(const Attend& a, hipStream_t st) {
-    hipLaunchKernelGGL((attend_kernel<DP, KB, VB, T>), dim3(a.blocks),
-                       dim3(kThreads), 0, st, a);
-    return hipGetLastError();
+    return launch(attend_kernel<DP, KB, VB, T>, a.blocks, kThreads, st, a);
 }
 
 template <int DP, int KB, int VB>

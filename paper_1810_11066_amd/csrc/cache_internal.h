@@ -100,6 +100,21 @@ struct Eight {
     }
 };
 
+// ---- kernel launch ---------------------------------------------------------
+
+template <typename P>
+struct Same {
+    using type = P;
+};
+// The arguments convert to the kernel's parameter types.
+template <typename... P>
+hipError_t launch(void (*fn)(P...), uint32_t blocks, uint32_t threads,
+                  hipStream_t st, typename Same<P>::type... args) {
+    void* argv[] = {(void*)&args...};
+    return hipLaunchKernel((const void*)fn, dim3(blocks), dim3(threads), argv,
+                           0, st);
+}
+
 // ---- launchers (each returns hipSuccess or the launch error) ---------------
 
 // Compute units of the current device (cached per device).
@@ -132,14 +147,8 @@ struct Attend {
 
 // Waves of a SIMD that the attention kernel for dp padded channels and a type
 // leaves room for (its registers), and workgroups of a CU.
-#ifndef BS_W128
-#define BS_W128 0
-#endif
-#ifndef BS_W64
-#define BS_W64 0
-#endif
 constexpr int attend_waves(int dp, int dtype) {
-    return (dp == 64 ? 4 + BS_W64 : dp == 128 ? 3 + BS_W128 : 2) - (dtype == kF32 ? 1 : 0);
+    return (dp == 64 ? 4 : dp == 128 ? 3 : 2) - (dtype == kF32 ? 1 : 0);
 }
 
 // Tokens of a unit: what the waves of a workgroup take in one step.
