@@ -18,13 +18,14 @@
 //
 // Codes become float16 without conversions.  For 16-bit calls a code's own bits
 // are the operand: as a float16 they are the subnormal c 2^-24, which the
-// matrix unit multiplies exactly (one byte permutation or mask for two codes).
-// 4-bit codes in the second nibble of a byte stay there and count 16 c; the
-// queries (keys) or the final outputs (values) of those channels take the 16
-// back.  float32 calls centre the codes: 0x6400 | c is 1024 + c, and one packed
-// subtraction of 1024 + centre (128 or 8) gives c' = c - centre exactly, so
-// that sums do not grow by the offset and cancel again.  With z' = z + centre s
-// (centre 0 where the codes are not centred) a value is s c' + z', and
+// matrix unit multiplies exactly (one byte permutation for two codes).  4-bit
+// codes are taken as 16 c: the unit aligns products by the operands' exponents,
+// and the leading zeros of a subnormal are bits that it loses of the sum (with
+// c as it is logits were off by 2 to 4 10^-6, now by 2 10^-7).  float32 calls
+// centre the codes: 0x6400 | c is 1024 + c, and one packed subtraction of 1024 +
+// centre (128; 8 of the 4-bit ones) gives c' = c - centre exactly, so that sums
+// do not grow by the offset and cancel again.  With z' = z + centre s (centre 0
+// where the codes are not centred) a value is s c' + z', and
 //   logit = scale (s (q . c') + z' sum q)
 //   out   = (sum_t w_t c'_t + sum_t p_t z'_t) / sum_t p_t,   w = p s.
 //
@@ -158,14 +159,7 @@ __device__ __forceinline__ uint32_t minus(uint32_t pair, _Float16 bias) {
                               __builtin_bit_cast(half2v, pair) - b);
 }
 
-// Two 4-bit codes, 16 bits apart: nibble N (0, 1: of the low byte) of x.
-template <int N, bool CENTRED>
-__device__ __forceinline__ uint32_t nibble_pair(uint32_t x) {
-    const uint32_t c = x & (N ? 0x00F000F0u : 0x000F000Fu);
-    if constexpr (!CENTRED) return c;
-    return minus(c | 0x64006400u, (_Float16)(N ? 1152.0f : 1032.0f));
-}
-// Two 8-bit codes: bytes A and B of the pair (hi, lo), lo's are 0..3.
+// Two codes, bytes A and B of the pair (hi, lo) of words, lo's are 0..3.
 template <int A, int B, bool CENTRED>
 __device__ __forceinline__ uint32_t byte_pair(uint32_t hi, uint32_t lo) {
     const uint32_t c =
@@ -173,67 +167,51 @@ __device__ __forceinline__ uint32_t byte_pair(uint32_t hi, uint32_t lo) {
     if constexpr (!CENTRED) return c;
     return minus(c | 0x64006400u, (_Float16)1152.0f);
 }
+// 4-bit codes as bytes 16 c: those in the low halves of 4 bytes (codes 0, 2, 4,
+// 6 of a word) and in the high ones (1, 3, 5, 7).
+__device__ __forceinline__ uint32_t low_nibbles(uint32_t x) {
+    return x << 4 & 0xF0F0F0F0u;
+}
+__device__ __forceinline__ uint32_t high_nibbles(uint32_t x) {
+    return x & 0xF0F0F0F0u;
+}
 
-// Channel-major operand of the keys: 8 codes of one token as 4 words of two
-// float16 each.  8 bits: x, y hold 4 codes each, in order.  4 bits: x holds 8
-// codes; the pairs are (0,4) (1,5) (2,6) (3,7), the second and fourth times 16.
+// Channel-major operand of the keys: 8 codes of one token.  8 bits: 4 in x, 4
+// in y, in order; 4 bits: all in x, in the order 0 2 4 6 1 3 5 7.
 template <int BITS, bool CENTRED>
 __device__ __forceinline__ half8v key_operand(uint32_t x, uint32_t y) {
-    u32x4 f;
-    if constexpr (BITS == 8) {
-        f[0] = byte_pair<0, 1, CENTRED>(x, x);
-        f[1] = byte_pair<2, 3, CENTRED>(x, x);
-        f[2] = byte_pair<0, 1, CENTRED>(y, y);
-        f[3] = byte_pair<2, 3, CENTRED>(y, y);
-    } else {
-        const uint32_t h = x >> 8;
-        f[0] = nibble_pair<0, CENTRED>(x);
-        f[1] = nibble_pair<1, CENTRED>(x);
-        f[2] = nibble_pair<0, CENTRED>(h);
-        f[3] = nibble_pair<1, CENTRED>(h);
+    if constexpr (BITS == 4) {
+        y = high_nibbles(x);
+        x = low_nibbles(x);
     }
+    const u32x4 f = {byte_pair<0, 1, CENTRED>(x, x),
+                     byte_pair<2, 3, CENTRED>(x, x),
+                     byte_pair<0, 1, CENTRED>(y, y),
+                     byte_pair<2, 3, CENTRED>(y, y)};
     return __builtin_bit_cast(half8v, f);
 }
-// Channel of element e (0..7) of that operand, and its factor.
+// Channel of element e (0..7) of that operand.
 template <int BITS>
 __device__ __forceinline__ constexpr int key_channel(int e) {
-    return BITS == 8 ? e : (e >> 1) + 4 * (e & 1);
-}
-template <int BITS>
-__device__ __forceinline__ constexpr float key_factor(int e) {
-    return BITS == 4 && ((e >> 1) & 1) ? 1.0f / 16.0f : 1.0f;
+    return BITS == 8 ? e : 2 * (e & 3) + (e >> 2);
 }
 
-// Token-major operands of the values: from 4 codes of each of 8 tokens (8
-// bits: a word each; 4 bits: the low half of a word each) one operand for each
-// of the 4 channels; of 4-bit codes channels 1 and 3 are times 16.
-template <int BITS, bool CENTRED>
+// Token-major operands of the values: from 4 codes, as bytes, of each of 8
+// tokens one operand for each of the 4 channels.
+template <bool CENTRED>
 __device__ __forceinline__ void value_operands(const uint32_t (&x)[8],
                                                half8v (&f)[4]) {
     u32x4 r[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const uint32_t a = x[2 * p], b = x[2 * p + 1];
-        if constexpr (BITS == 8) {
-            r[0][p] = byte_pair<0, 4, CENTRED>(b, a);
-            r[1][p] = byte_pair<1, 5, CENTRED>(b, a);
-            r[2][p] = byte_pair<2, 6, CENTRED>(b, a);
-            r[3][p] = byte_pair<3, 7, CENTRED>(b, a);
-        } else {
-            const uint32_t v = __builtin_amdgcn_perm(b, a, 0x05040100u);
-            const uint32_t h = v >> 8;
-            r[0][p] = nibble_pair<0, CENTRED>(v);
-            r[1][p] = nibble_pair<1, CENTRED>(v);
-            r[2][p] = nibble_pair<0, CENTRED>(h);
-            r[3][p] = nibble_pair<1, CENTRED>(h);
-        }
+        r[0][p] = byte_pair<0, 4, CENTRED>(b, a);
+        r[1][p] = byte_pair<1, 5, CENTRED>(b, a);
+        r[2][p] = byte_pair<2, 6, CENTRED>(b, a);
+        r[3][p] = byte_pair<3, 7, CENTRED>(b, a);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = __builtin_bit_cast(half8v, r[i]);
-}
-template <int BITS>
-__device__ __forceinline__ constexpr float value_factor(int channel) {
-    return BITS == 4 && (channel & 1) ? 1.0f / 16.0f : 1.0f;
 }
 
 __device__ __forceinline__ f32x4 mfma(half8v a, half8v b, f32x4 c) {
@@ -343,8 +321,10 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
     constexpr bool kTwoQ = T == kF32, kTwoW = T != kBF16, kCentred = T == kF32;
     constexpr float kCentreK = !kCentred ? 0.0f : KB == 8 ? 128.0f : 8.0f;
     constexpr float kCentreV = !kCentred ? 0.0f : VB == 8 ? 128.0f : 8.0f;
-    // what a code's bits stand for as float16
+    // codes over what they are as float16
     constexpr float kCode = kCentred ? 1.0f : 0x1p24f;
+    constexpr float kCodeK = KB == 8 ? kCode : kCode / 16;
+    constexpr float kCodeV = VB == 8 ? kCode : kCode / 16;
     __shared__ float sm_o[kWaves][16][DP + 4];
     __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
 
@@ -550,14 +530,12 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
                 for (int j = 0; j < 8; ++j) {
                     const float y = qx[i].get(key_channel<KB>(j)) * down;
                     const _Float16 hi = (_Float16)y;
-                    q_hi[i][j] = hi * (_Float16)key_factor<KB>(j);
-                    if constexpr (kTwoQ)
-                        q_lo[i][j] = (_Float16)((y - (float)hi) *
-                                                key_factor<KB>(j));
+                    q_hi[i][j] = hi;
+                    if constexpr (kTwoQ) q_lo[i][j] = (_Float16)(y - (float)hi);
                 }
             // (above 0, so that a masked -inf stays one)
-            q_scale = fmaxf(fabsf(a.scale2) * ldexpf(kCode, e), 1e-30f);
-            q_sum = sum * down * (1.0f / kCode);
+            q_scale = fmaxf(fabsf(a.scale2) * ldexpf(kCodeK, e), 1e-30f);
+            q_sum = sum * down * (1.0f / kCodeK);
         }
 
         f32x4 o[kOwn];
@@ -670,19 +648,44 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
             if (more) load_steps(next);
 
             // ---- values
-#pragma unroll
-            for (int j = 0; j < kOwn; j += 4) {
-                uint32_t y[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    y[i] = VB == 8 ? codes.v[i][j >> 2]
-                                   : codes.v[i][j >> 3] >> 16 * ((j >> 2) & 1);
+            auto add_values = [&](const uint32_t (&y)[8], int first, int by) {
                 half8v f[4];
-                value_operands<VB, kCentred>(y, f);
+                value_operands<kCentred>(y, f);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    o[j + e] = mfma(f[e], w_hi, o[j + e]);
-                    if constexpr (kTwoW) o[j + e] = mfma(f[e], w_lo, o[j + e]);
+                    f32x4& sum = o[first + e * by];
+                    sum = mfma(f[e], w_hi, sum);
+                    if constexpr (kTwoW) sum = mfma(f[e], w_lo, sum);
+                }
+            };
+            if constexpr (VB == 8) {
+#pragma unroll
+                for (int j = 0; j < kOwn; j += 4) {
+                    uint32_t y[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = codes.v[i][j >> 2];
+                    add_values(y, j, 1);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < kOwn; j += 8) {
+                    uint32_t y[8], z[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        y[i] = low_nibbles(codes.v[i][j >> 3]);
+                        z[i] = high_nibbles(codes.v[i][j >> 3]);
+                    }
+                    if constexpr (kOwn >= 8) {
+                        add_values(y, j, 2);         // channels 0, 2, 4, 6
+                        add_values(z, j + 1, 2);     // 1, 3, 5, 7
+                    } else {
+                        // 4 codes: bytes 0 and 1 of each
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            y[i] = __builtin_amdgcn_perm(z[i], y[i],
+                                                         0x05010400u);
+                        add_values(y, j, 1);
+                    }
                 }
             }
             if (more) {
@@ -710,7 +713,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     r[e] = __builtin_fmaf(
-                        o[j + e][i], value_factor<VB>(j + e) * kCode, sum_z);
+                        o[j + e][i], kCodeV, sum_z);
                 *reinterpret_cast<f32x4*>(
                     &sm_o[wave][col][kOwn * (4 * quarter + i) + j]) = r;
             }
