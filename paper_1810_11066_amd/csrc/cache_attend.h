@@ -276,20 +276,25 @@ __device__ __forceinline__ Rsrc rows_buffer(const void* base, int64_t at,
         const_cast<uint8_t*>(static_cast<const uint8_t*>(base)) + at, (short)0,
         bytes, 0x00020000);   // 32-bit data format
 }
-// N words from a 4 N-byte aligned offset.
-template <int N>
+// N words from a 4 N-byte aligned offset.  Rows of 8-bit values are read with
+// the non-temporal policy: one instruction takes whole lines of them, and they
+// leave the caches to the rest (100 sequences of 500-3000 tokens 85 -> 79 us).
+// Keys and 4-bit values come by two instructions a line, and the second one
+// would often find it gone (128 x 12-16 Ki tokens, 4-bit values 518 -> 538 us).
+constexpr int kOnce = 2;
+template <int POLICY, int N>
 __device__ __forceinline__ void load_words(Rsrc rows, uint32_t at,
                                            uint32_t (&w)[N]) {
     if constexpr (N == 1) {
-        w[0] = __builtin_amdgcn_raw_buffer_load_b32(rows, at, 0, 0);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b32(rows, at, 0, POLICY);
     } else if constexpr (N == 2) {
         const u32x2 t = __builtin_bit_cast(
-            u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, 0));
+            u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, POLICY));
         w[0] = t[0], w[1] = t[1];
     } else {
         static_assert(N == 4);
         const u32x4 t = __builtin_bit_cast(
-            u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, 0));
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, POLICY));
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = t[i];
     }
@@ -450,15 +455,15 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
                     rows_buffer(a.c.codes[0], t.row[s] * k_row, 16 * k_row);
 #pragma unroll
                 for (int j = 0; j < C::kChunks; ++j)
-                    load_words(rows, k_at[j], codes.k[s][j]);
+                    load_words<0>(rows, k_at[j], codes.k[s][j]);
             }
         };
         auto load_steps = [&](const Tile& t) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                load_words(rows_buffer(a.c.steps[0], t.row[s] * 4, 64),
+                load_words<0>(rows_buffer(a.c.steps[0], t.row[s] * 4, 64),
                            16 * group, ks[s]);
-                load_words(rows_buffer(a.c.steps[1], t.row[s] * 4, 64),
+                load_words<0>(rows_buffer(a.c.steps[1], t.row[s] * 4, 64),
                            16 * group, vs[s]);
             }
         };
@@ -475,7 +480,8 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
                             __builtin_amdgcn_raw_buffer_load_b16(rows, at, 0,
                                                                  0);
                     else
-                        load_words(rows, at, codes.v[4 * s + i]);
+                        load_words<VB == 8 ? kOnce : 0>(rows, at,
+                                                        codes.v[4 * s + i]);
                 }
             }
         };
