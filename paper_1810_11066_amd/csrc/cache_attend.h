@@ -2,7 +2,8 @@
 //
 // A workgroup takes units of 128 tokens of one (sequence, key-value head, tile
 // of up to 16 query heads); its four waves take 32 tokens of a unit each and
-// never wait for one another until the segment ends.  Per wave and unit:
+// never wait for one another until the pair ends.  (The wide form is as many
+// waves as a CU holds, and units of 32 tokens for each.)  Per wave and unit:
 //
 //   logits  S[token][head] = K q as v_mfma_f32_16x16x32_f16 with the codes as
 //           the A operand (row = token, k = channel) and the queries as B
@@ -21,7 +22,7 @@
 // matrix unit multiplies exactly (one byte permutation for two codes).  4-bit
 // codes are taken as 16 c: the unit aligns products by the operands' exponents,
 // and the leading zeros of a subnormal are bits that it loses of the sum (with
-// c as it is logits were off by 2 to 4 10^-6, now by 2 10^-7).  float32 calls
+// c as it is lse was off by 2 to 4 10^-6, now by up to 4 10^-7).  float32 calls
 // centre the codes: 0x6400 | c is 1024 + c, and one packed subtraction of 1024 +
 // centre (128; 8 of the 4-bit ones) gives c' = c - centre exactly, so that sums
 // do not grow by the offset and cancel again.  With z' = z + centre s (centre 0
@@ -60,8 +61,6 @@
 
 namespace bscache {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
 constexpr float kNone = -3.0e38f;       // maximum of no logits
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -73,8 +72,8 @@ struct Span {
     int32_t length, first;
     __device__ __forceinline__ int32_t start() const { return first & ~15; }
     // a sequence without tokens has one unit: somebody writes its zeros
-    __device__ __forceinline__ int32_t units() const {
-        const int32_t n = (length - start() + kUnit - 1) / kUnit;
+    __device__ __forceinline__ int32_t units(int32_t tokens = kUnit) const {
+        const int32_t n = (length - start() + tokens - 1) / tokens;
         return n > 1 ? n : 1;
     }
 };
@@ -317,10 +316,14 @@ struct Tile {
     int32_t end[2];
 };
 
-template <int DP, int KB, int VB, int T>
-__global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
-    const Attend a) {
+template <int DP, int KB, int VB, int T, bool WIDE>
+__global__ __launch_bounds__(64 * group_waves(DP, T, WIDE),
+                             attend_waves(DP, T))
+void attend_kernel(const Attend a) {
     using C = Codes<DP, KB, VB>;
+    constexpr int kWaves = group_waves(DP, T, WIDE), kThreads = 64 * kWaves;
+    constexpr int kStep = 32 * kWaves;          // tokens of a workgroup's step
+    const bool one = WIDE || a.whole;           // every pair one workgroup's
     constexpr int kSteps = DP / 32;             // MFMAs of the logits
     constexpr int kOwn = C::kOwn;
     constexpr bool kTwoQ = T == kF32, kTwoW = T != kBF16, kCentred = T == kF32;
@@ -343,7 +346,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
     int32_t place = 0, place_end = 0, pair_start = 0, seq = 0, pair = 0;
     // lengths of 64 sequences, from `lengths_of` on
     int32_t lengths = 0, lengths_of = 0;
-    if (a.whole) {
+    if (one) {
         seq = self / pairs;
         pair = self - seq * pairs;
         lengths = uniform_load(a.lengths, seq);
@@ -387,10 +390,10 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
         }
         const Span span = span_of(
             a, __builtin_amdgcn_readlane(lengths, seq - lengths_of));
-        const int32_t units = span.units();
+        const int32_t units = span.units(kStep);
         // units [c0, c1) of this pair
         int32_t c0 = 0, c1 = units;
-        if (!a.whole) {
+        if (!one) {
             c0 = min(place - pair_start, units);
             c1 = min(place_end - pair_start, units);
             pair_start += pair_places(units);
@@ -403,7 +406,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
             pair = 0;
             ++seq;
         }
-        const bool last = a.whole || place >= place_end;
+        const bool last = one || place >= place_end;
         if (c0 >= c1) {              // nothing but empty places
             if (last) break;
             continue;
@@ -434,7 +437,7 @@ __global__ __launch_bounds__(kThreads, attend_waves(DP, T)) void attend_kernel(
         const int64_t table = (int64_t)now_seq * a.max_pages;
         auto find = [&](int32_t c) {
             Tile t;
-            t.token = span.start() + c * kUnit + wave * 32;
+            t.token = span.start() + c * kStep + wave * 32;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const int32_t at = t.token + 16 * s;

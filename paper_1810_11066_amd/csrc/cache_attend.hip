@@ -14,7 +14,7 @@ namespace {
 // rows that take every rows-th partial result and are added at the end; a
 // thread has kDeep of them in flight, and a running maximum of its own, so
 // that no load waits for another but the lengths'.
-constexpr int kDeep = 8;
+constexpr int kDeep = 8, kThreads = 256;
 
 __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a,
                                                         int32_t few) {
@@ -118,21 +118,38 @@ template <> hipError_t launch_attend_dp<64>(const Attend&, hipStream_t);
 template <> hipError_t launch_attend_dp<128>(const Attend&, hipStream_t);
 template <> hipError_t launch_attend_dp<256>(const Attend&, hipStream_t);
 
+// How a call is shared out, by what the host knows: the pairs of sequences and
+// head tiles, and the tokens that the longest sequence may span.
+//
 // A pair to one workgroup needs no plan of the lengths and no join (4.4 us and a
-// launch), but the longest sequence sets the time: about 1 us a unit and 4.5 us
-// besides.  (us a pass, pairs whole / shared: 8 pairs of 4 units 8.9 / 9.7, of 8
-// units 13.1 / 10.6; 512 pairs of 8 units 33 / 41, of 16 units 34 / 40, where
-// the GPU is full either way.)  So: up to 4 units always, up to 16 where there
-// are pairs for half of the workgroups that run at once -- there a batch with
-// one long sequence among short ones loses at most the 16 us of its units.
-void plan_attend(Attend& a, int64_t units) {
+// launch), but the longest pair sets the time: 4.5 us and 1 us a unit of 128
+// tokens.  Up to 4 units that is always shorter (8 pairs of 4 units 8.9 us whole
+// and 9.7 shared, of 8 units 13.1 and 10.6).  Longer ones win where the pairs
+// fill the GPU anyway: up to 8 units with a pair for every CU (320 pairs of 8
+// units 22 and 25 us), up to 16 with pairs for half of the workgroups that run
+// at once (512 pairs of 16 units, 64 channels 32 and 40 us); a batch with one
+// long sequence among short ones loses at most the time of those units.
+//
+// With fewer pairs than CUs a workgroup can have its CU to itself: the wide
+// form, of as many waves as the CU holds (8 to 16).  A CU's own rate of reading
+// bounds it, so it needs pairs on a quarter of the CUs, and sequences of more
+// than 4 units that it takes in 4 steps (128 pairs of 700 tokens 11.3 us wide,
+// 15.1 shared; of 1024 13.4 and 17.8; of 2048 no difference; 8 pairs of 800
+// tokens 12.2 and 10.6).
+//
+// Everything else is shared: as many workgroups as run at once, each with its
+// part (4 times as many, taken up as others end: 551 us for 524 at 128
+// sequences of 12-16 Ki tokens).
+void plan_attend(Attend& a, int64_t tokens) {
     const int64_t pairs = (int64_t)a.batch * a.c.kv_heads * a.head_tiles;
     const int dp = a.c.dim > 128 ? 256 : a.c.dim > 64 ? 128 : 64;
-    const int64_t at_once = (int64_t)device_cus() * attend_waves(dp, a.dtype);
-    a.whole = units <= 4 || (units <= 16 && 2 * pairs >= at_once);
-    // shared units: as many workgroups as run at once, each with its part (4
-    // times as many, taken up as others end: 524 -> 551 us at 128 sequences of
-    // 12-16 Ki tokens)
+    const int waves = attend_waves(dp, a.dtype);
+    const int64_t units = (tokens + kUnit - 1) / kUnit;
+    const int64_t cus = device_cus(), at_once = cus * waves;
+    a.wide = waves > 1 && pairs <= cus && 4 * pairs >= cus && units > 4 &&
+             tokens <= 4 * 32 * group_waves(dp, a.dtype, true);
+    a.whole = a.wide || units <= 4 || (units <= 8 && pairs >= cus) ||
+              (units <= 16 && 2 * pairs >= at_once);
     const int64_t n = a.whole ? pairs : std::min(pairs * units, at_once);
     a.blocks = (int32_t)std::max(n, (int64_t)1);
 }

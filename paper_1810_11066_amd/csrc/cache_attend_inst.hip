@@ -7,7 +7,12 @@ namespace {
 
 template <int DP, int KB, int VB, int T>
 hipError_t go(const Attend& a, hipStream_t st) {
-    return launch(attend_kernel<DP, KB, VB, T>, a.blocks, kThreads, st, a);
+    if constexpr (attend_waves(DP, T) > 1)
+        if (a.wide)
+            return launch(attend_kernel<DP, KB, VB, T, true>, a.blocks,
+                          64 * group_waves(DP, T, true), st, a);
+    return launch(attend_kernel<DP, KB, VB, T, false>, a.blocks,
+                  64 * group_waves(DP, T, false), st, a);
 }
 
 template <int DP, int KB, int VB>

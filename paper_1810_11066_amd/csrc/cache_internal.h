@@ -142,6 +142,7 @@ struct Attend {
     int32_t max_pages, max_len, window, dtype;
     float scale2;             // scale log2(e)
     bool whole;               // every pair is one workgroup's
+    bool wide;                // of as many waves as a CU holds (whole too)
     int32_t blocks;           // workgroups
 };
 
@@ -151,12 +152,17 @@ constexpr int attend_waves(int dp, int dtype) {
     return (dp == 64 ? 4 : dp == 128 ? 3 : 2) - (dtype == kF32 ? 1 : 0);
 }
 
-// Tokens of a unit: what the waves of a workgroup take in one step.
+// Waves of a workgroup: 4, or all that a CU holds.
+constexpr int group_waves(int dp, int dtype, bool wide) {
+    return wide ? 4 * attend_waves(dp, dtype) : 4;
+}
+
+// Tokens of a unit: what the 4 waves of a workgroup take in one step.
 constexpr int kUnit = 128;
 
-// Chooses `whole` and `blocks` for a call whose longest sequence has `units`
-// units.
-void plan_attend(Attend& a, int64_t units);
+// Chooses `whole`, `wide` and `blocks` for a call whose longest sequence spans
+// `tokens` tokens.
+void plan_attend(Attend& a, int64_t tokens);
 
 hipError_t launch_attend(const Attend& a, hipStream_t st);
 

@@ -44,19 +44,35 @@ def split_codes(b, bits):
     return np.stack([b & 15, b >> 4], -1).reshape(b.shape[:-1] + (-1,))
 
 
+def error_terms(kind, dim, tokens):
+    """(binary32 roundings of a logit's magnitudes, relative error of a weight
+    times s, relative error of a sum over tokens) that a call may have.
+
+    A logit is s (q . c') + z' sum q, z' = z + centre s, with the codes c' = c -
+    centre (centre 0 for 16-bit calls, 128 or 8 for float32).  Its dim products
+    are added in binary32, in the matrix unit's order: at most dim roundings of
+    2^-24 of the magnitudes added, and 16 for the rest of the expression;
+    16-bit calls multiply subnormals of 8 bits, which lie up to 2 bits below
+    what the unit aligns them as, so 4 times that.  A float32 query is kept to
+    22 bits.  A weight times s is kept to 11 bits for bfloat16 calls, to 22 for
+    the others.  Tokens accumulate in binary32: at most tokens / 32 + 64
+    roundings in a row (again 4 times for subnormals), and what is below the
+    smallest float16 of a weight, 2^-30 of the largest."""
+    unit = 2.0 ** -24
+    wide = 1 if kind == "f32" else 4
+    logit = wide * unit * (dim + 16) + (2.0 ** -22 if kind == "f32" else 0.0)
+    weight = 2.0 ** -11 if kind == "bf16" else 2.0 ** -22
+    return logit, weight, wide * unit * (tokens / 32 + 64) + 2.0 ** -30
+
+
+def centre(kind, bits):
+    return 0 if kind != "f32" else 128 if bits == 8 else 8
+
+
 def attention(q, c_k, s_k, z_k, c_v, s_v, z_v, scale, kbits, vbits, kind):
     """One head: q [dim], codes [tokens][dim], steps [tokens]; (out, lse, how
-    far out may be off, how far lse may be off), all float64.
-
-    Errors: a product sum is kept in binary32 as s (q . c') + z' sum q with
-    centred codes c' (|c'| <= 128 or 8) and z' = z + centre s, so a logit is
-    off by a few units of binary32 of the magnitudes added, M = scale (s |q| .
-    |c'| + |z'| sum |q|): dim / 4 accumulations in the matrix unit's order are
-    at most dim roundings of 2^-24; a float32 query is kept to 22 bits.  A
-    logit off by d moves a weight by a factor e^d; both the sum and the total
-    move.  A weight times s is rounded to 11 bits (float32 calls: 22), tokens
-    accumulate in binary32: at most (tokens / 32 + 64) roundings in a row, of
-    sums of w |c'| and p |z'|."""
+    far out may be off, how far lse may be off), all float64.  A logit off by d
+    moves a weight by a factor e^d; both the sum and the total move."""
     q = q.astype(np.float64)
     dim = q.size
     if len(s_k) == 0:
@@ -64,7 +80,7 @@ def attention(q, c_k, s_k, z_k, c_v, s_v, z_v, scale, kbits, vbits, kind):
     ck, cv = c_k.astype(np.float64), c_v.astype(np.float64)
     s_k, z_k = s_k.astype(np.float64)[:, None], z_k.astype(np.float64)[:, None]
     s_v, z_v = s_v.astype(np.float64)[:, None], z_v.astype(np.float64)[:, None]
-    mk, mv = (128 if kbits == 8 else 8), (128 if vbits == 8 else 8)
+    mk, mv = centre(kind, kbits), centre(kind, vbits)
     k, v = z_k + s_k * ck, z_v + s_v * cv
     logit = scale * (k @ q)
     top = logit.max()
@@ -74,13 +90,9 @@ def attention(q, c_k, s_k, z_k, c_v, s_v, z_v, scale, kbits, vbits, kind):
     lse = top + np.log(total)
     size = abs(scale) * (s_k[:, 0] * (np.abs(ck - mk) @ np.abs(q)) +
                          np.abs(z_k + mk * s_k)[:, 0] * np.abs(q).sum())
+    by_logit, by_weight, by_sum = error_terms(kind, dim, len(p))
     unit = 2.0 ** -24
-    d = (size * unit * (dim + 16)).max() + \
-        np.abs(logit).max() * 8 * unit + \
-        (size * 2.0 ** -22).max() * (kind == "f32")
+    d = size.max() * by_logit + np.abs(logit).max() * 8 * unit
     spread = p @ (s_v * np.abs(cv - mv) + np.abs(z_v + mv * s_v)) / total
-    w = 2.0 ** -22 if kind == "f32" else 2.0 ** -11
-    sums = (len(p) / 32 + 64) * unit
-    # 2^-30 of the largest: weights below the smallest float16
-    tol = STEP[kind] * np.abs(out) + spread * (w + 2 * d + sums + 2.0 ** -30)
-    return out, lse, tol, d + sums + 4 * unit * abs(lse)
+    tol = STEP[kind] * np.abs(out) + spread * (by_weight + 2 * d + by_sum)
+    return out, lse, tol, d + by_sum + 4 * unit * abs(lse)

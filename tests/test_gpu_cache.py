@@ -629,3 +629,69 @@ def test_memory_around_the_outputs_stays():
         torch.cuda.current_stream().cuda_stream) == kc.OK
     torch.cuda.synchronize()
     assert np.array_equal(host(got).reshape(want.shape), want)
+
+
+@pytest.mark.parametrize("batch,longest", [
+    (1, 500), (1, 700),         # whole pairs of up to 4 units; shared ones
+    (12, 700), (20, 1500),      # wide workgroups, and what is past their 4 steps
+    (50, 1000), (60, 1100),     # pairs on every CU: whole up to 8 units
+    (70, 2000), (70, 2100)])    # many pairs: whole up to 16
+@pytest.mark.parametrize("dim,kind", [(64, "bf16"), (128, "f16"),
+                                      (256, "bf16"), (96, "f32")])
+def test_attend_on_both_sides_of_the_plan(batch, longest, dim, kind):
+    """Ways of sharing a call out, each at its bounds: lengths up to the longest
+    one, against float64 on the GPU."""
+    say(batch, longest, dim, kind)
+    gen = torch.Generator(device="cuda").manual_seed(batch + longest)
+    kv, group, page = 8, 2, 32
+    pages = 200
+    cache = kc.empty(pages, kv, page, dim, 8, 4)
+    k, v = (torch.randn((pages * page, kv, dim), generator=gen, device="cuda")
+            for _ in range(2))
+    kc.write(k, v, torch.arange(pages * page, dtype=torch.int32,
+                                device="cuda"), cache)
+    # rows as offset and rest: value = s c' + z', both float64
+    rest, offset = [], []
+    for x, steps, bits in zip(kc.read(torch.arange(
+            pages * page, dtype=torch.int32, device="cuda"), cache, dim),
+            (cache.k_steps, cache.v_steps), (8, 4)):
+        s, z = steps.double().transpose(1, 2).reshape(-1, kv, 2).unbind(-1)
+        offset.append((z + ref.centre(kind, bits) * s)[..., None])
+        rest.append(x.double() - offset[-1])
+    table = torch.randint(pages, (batch, -(-longest // page)), generator=gen,
+                          device="cuda", dtype=torch.int32)
+    lengths = torch.randint(longest + 1, (batch,), generator=gen,
+                            device="cuda", dtype=torch.int32)
+    lengths[0] = longest
+    if batch > 1:
+        lengths[1] = 0
+    q = torch.randn((batch, kv * group, dim), generator=gen,
+                    device="cuda").to(DTYPE[kind])
+    out, lse = kc.attend(q, cache, table, lengths, max_len=longest)
+    for b in range(batch):
+        n = int(lengths[b])
+        t = torch.arange(n, device="cuda")
+        slot = table[b].long()[t // page] * page + t % page
+        if n == 0:
+            assert (out[b] == 0).all() and (lse[b] == -torch.inf).all()
+            continue
+        # (n, kv, dim) -> (kv, dim, n) and (kv, n, dim), contiguous
+        kr, kz = (x[0][slot].permute(1, 2, 0).contiguous()
+                  for x in (rest, offset))
+        vr, vz = (x[1][slot].permute(1, 0, 2).contiguous()
+                  for x in (rest, offset))
+        qb = q[b].double().view(kv, group, dim)
+        x = torch.matmul(qb, kr + kz) * dim ** -0.5
+        p = torch.softmax(x, -1)
+        want = torch.matmul(p, vr + vz).view(kv * group, dim)
+        size = dim ** -0.5 * (torch.matmul(qb.abs(), kr.abs()) +
+                              qb.abs().sum(-1, keepdim=True) * kz.abs())
+        by_logit, by_weight, by_sum = ref.error_terms(kind, dim, n)
+        d = float(size.max() * by_logit + x.abs().max() * 2.0 ** -21)
+        spread = torch.matmul(p, vr.abs() + vz.abs()).view(kv * group, dim)
+        tol = ref.STEP[kind] * want.abs() + \
+            spread * (by_weight + 2 * d + by_sum)
+        assert ((out[b].double() - want).abs() <= tol).all(), (b, n)
+        total = torch.logsumexp(x, -1).view(-1)
+        far = (lse[b].double() - total).abs()
+        assert (far <= d + by_sum + 2.0 ** -22 * total.abs()).all(), (b, n)
