@@ -165,6 +165,16 @@ bscache_status bscache_attend(const bscache_pages *cache,
                               int64_t workspace_bytes,
                               bscache_stream_t stream);
 
+/* Describes, as text, the kernel and launch that bscache_attend would use (the
+ * way the call is shared out, workgroups, waves of each, workspace bytes).
+ * Writes at most len bytes including the terminating NUL into buf (truncating);
+ * host only, nothing is enqueued, the cache's pointers are not looked at.
+ * Errors: as bscache_attend's checks of sizes; INVALID_ARG for a NULL buf or
+ * len < 1. */
+bscache_status bscache_attend_describe(const bscache_pages *cache,
+                                       const bscache_attend_params *p,
+                                       char *buf, int32_t len);
+
 /* Detail of the last non-OK status returned on the calling thread ("" if
  * none).  The string stays valid until the next call on that thread. */
 const char *bscache_last_error(void);

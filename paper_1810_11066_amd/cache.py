@@ -38,8 +38,8 @@ ERR_UNSUPPORTED = 2
 ERR_HIP = 4
 
 EXPORTED = ("bscache_write", "bscache_read", "bscache_attend",
-            "bscache_attend_workspace", "bscache_last_error",
-            "bscache_abi_version")
+            "bscache_attend_workspace", "bscache_attend_describe",
+            "bscache_last_error", "bscache_abi_version")
 
 # bscache_dtype
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -86,6 +86,7 @@ def load_library():
             "bscache_write": (ci, [S, P, P, i64, i64, ci, P, i64, P]),
             "bscache_read": (ci, [S, P, i64, P, P, ci, P]),
             "bscache_attend_workspace": (ci, [S, S, ctypes.POINTER(i64)]),
+            "bscache_attend_describe": (ci, [S, S, P, ctypes.c_int32]),
             "bscache_attend": (ci, [S, S, P, P, P, P, P, P, i64, P]),
             "bscache_last_error": (ctypes.c_char_p, []),
             "bscache_abi_version": (ci, []),
@@ -355,3 +356,16 @@ def attend(q: torch.Tensor, cache, table: torch.Tensor, lengths: torch.Tensor,
           lse.data_ptr(), space.data_ptr() if need else None, need,
           _stream(device))
     return out, lse
+
+
+def describe(pages: int, kv_heads: int, page_tokens: int, dim: int,
+             batch: int, heads: int, max_len: int, kbits: int = 8,
+             vbits: int = 8, window: int = 0, dtype=torch.bfloat16) -> str:
+    """Kernel and launch that attend would use for these sizes (host only)."""
+    buf = ctypes.create_string_buffer(256)
+    _check(load_library().bscache_attend_describe(
+        _PAGES.pack(pages, kv_heads, page_tokens, dim, kbits, vbits, 0, 0, 0,
+                    0),
+        _PARAMS.pack(heads * dim, batch, heads, -(-max_len // page_tokens),
+                     max_len, window, _DTYPES[dtype], 1.0), buf, 256))
+    return buf.value.decode()

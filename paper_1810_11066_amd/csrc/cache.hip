@@ -618,6 +618,28 @@ bscache_status bscache_attend_workspace(const bscache_pages* cache,
     return st == BSCACHE_OK ? ok() : st;
 }
 
+bscache_status bscache_attend_describe(const bscache_pages* cache,
+                                       const bscache_attend_params* p,
+                                       char* buf, int32_t len) {
+    if (!buf || len < 1) return fail(BSCACHE_ERR_INVALID_ARG, "buf/len");
+    buf[0] = '\0';
+    bscache::Attend a;
+    int64_t bytes;
+    const bscache_status st =
+        check_attend(cache, p, &a, nullptr, false, &bytes);
+    if (st != BSCACHE_OK) return st;
+    const int dp = bscache::padded_dim(a.c.dim);
+    snprintf(buf, (size_t)len,
+             "attend_kernel<%d, %d, %d, %s> %s grid=%d waves=%d workspace=%lld",
+             dp, a.c.bits[0], a.c.bits[1],
+             a.dtype == bscache::kF32   ? "f32"
+             : a.dtype == bscache::kF16 ? "f16"
+                                        : "bf16",
+             a.wide ? "wide" : a.whole ? "whole" : "shared", a.blocks,
+             bscache::group_waves(dp, a.dtype, a.wide), (long long)bytes);
+    return ok();
+}
+
 bscache_status bscache_attend(const bscache_pages* cache,
                               const bscache_attend_params* p, const void* q,
                               const int32_t* table, const int32_t* lengths,

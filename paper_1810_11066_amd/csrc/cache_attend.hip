@@ -142,7 +142,7 @@ template <> hipError_t launch_attend_dp<256>(const Attend&, hipStream_t);
 // sequences of 12-16 Ki tokens).
 void plan_attend(Attend& a, int64_t tokens) {
     const int64_t pairs = (int64_t)a.batch * a.c.kv_heads * a.head_tiles;
-    const int dp = a.c.dim > 128 ? 256 : a.c.dim > 64 ? 128 : 64;
+    const int dp = padded_dim(a.c.dim);
     const int waves = attend_waves(dp, a.dtype);
     const int64_t units = (tokens + kUnit - 1) / kUnit;
     const int64_t cus = device_cus(), at_once = cus * waves;
@@ -155,9 +155,10 @@ void plan_attend(Attend& a, int64_t tokens) {
 }
 
 hipError_t launch_attend(const Attend& a, hipStream_t st) {
-    const hipError_t e = a.c.dim > 128  ? launch_attend_dp<256>(a, st)
-                         : a.c.dim > 64 ? launch_attend_dp<128>(a, st)
-                                        : launch_attend_dp<64>(a, st);
+    const int dp = padded_dim(a.c.dim);
+    const hipError_t e = dp == 256   ? launch_attend_dp<256>(a, st)
+                         : dp == 128 ? launch_attend_dp<128>(a, st)
+                                     : launch_attend_dp<64>(a, st);
     if (e != hipSuccess || a.whole) return e;
     const int32_t pairs = a.batch * a.c.kv_heads * a.head_tiles;
     const int32_t heads = std::min(a.group, 16);

@@ -146,6 +146,11 @@ struct Attend {
     int32_t blocks;           // workgroups
 };
 
+// Channels that the attention kernel for a row of dim channels is made for.
+constexpr int padded_dim(int dim) {
+    return dim > 128 ? 256 : dim > 64 ? 128 : 64;
+}
+
 // Waves of a SIMD that the attention kernel for dp padded channels and a type
 // leaves room for (its registers), and workgroups of a CU.
 constexpr int attend_waves(int dp, int dtype) {

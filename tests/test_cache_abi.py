@@ -178,6 +178,60 @@ def test_workspace(lib):
     assert most[0] == most[1] == most[2]
 
 
+# ---- the plan (256 compute units where there is no GPU) ---------------------
+
+def plan(batch, max_len, kv_heads=8, dim=128, group=4, **kw):
+    d = kc.describe(100, kv_heads, 32, dim, batch, kv_heads * group, max_len,
+                    **kw)
+    m = re.match(r"attend_kernel<(\d+), (\d), (\d), (\w+)> (\w+) grid=(\d+) "
+                 r"waves=(\d+) workspace=(\d+)$", d)
+    assert m, d
+    return m.group(5), int(m.group(6)), int(m.group(7)), int(m.group(8))
+
+
+@pytest.mark.parametrize("batch,max_len,way,grid,waves", [
+    (1, 512, "whole", 8, 4), (1, 513, "shared", 40, 4),
+    (1, 100000, "shared", 768, 4),
+    # wide: pairs on a quarter of the CUs up to all, 5 units to 4 steps
+    (7, 700, "shared", 336, 4), (8, 700, "wide", 64, 12),
+    (8, 512, "whole", 64, 4), (8, 1536, "wide", 64, 12),
+    (8, 1537, "shared", 768, 4), (32, 1024, "wide", 256, 12),
+    # whole: 8 units with a pair for every CU, 16 with pairs for half of the
+    # workgroups that run at once
+    (33, 1024, "whole", 264, 4), (33, 1025, "shared", 768, 4),
+    (47, 1025, "shared", 768, 4), (48, 1025, "whole", 384, 4),
+    (48, 2048, "whole", 384, 4), (48, 2049, "shared", 768, 4)])
+def test_plan_rules(batch, max_len, way, grid, waves):
+    w, g, n, space = plan(batch, max_len)
+    assert (w, g, n) == (way, grid, waves)
+    assert space == (grid * 2 * 16 * (128 + 2) * 4 if way == "shared" else 0)
+
+
+def test_plan_follows_registers_window_and_head_tiles():
+    # waves of a wide workgroup are what the kernel's registers leave room for
+    assert plan(16, 700, dim=64)[:3] == ("wide", 128, 16)
+    assert plan(16, 700, dim=256)[:3] == ("wide", 128, 8)
+    assert plan(16, 700, dtype=torch.float32)[:3] == ("wide", 128, 8)
+    # (one workgroup of 4 waves is all that runs on a CU at once)
+    assert plan(16, 700, dim=256, dtype=torch.float32)[:3] == ("whole", 128, 4)
+    # a window bounds the span: its first token is taken down to a 16
+    assert plan(1, 100000, window=497)[0] == "whole"
+    assert plan(1, 100000, window=498)[0] == "shared"
+    # 17 heads to a key-value head are two tiles
+    assert plan(1, 512, group=16)[1] == 8
+    assert plan(1, 512, group=17)[1] == 16
+
+
+def test_describe_validation(lib):
+    buf = ctypes.create_string_buffer(16)
+    assert lib.bscache_attend_describe(pages(), params(), None, 16) == INVALID
+    assert lib.bscache_attend_describe(pages(), params(), buf, 0) == INVALID
+    assert lib.bscache_attend_describe(pages(dim=24), params(), buf,
+                                       16) == UNSUPPORTED
+    assert lib.bscache_attend_describe(pages(), params(), buf, 16) == kc.OK
+    assert buf.value == b"attend_kernel<6"      # truncated
+
+
 # ---- the binding ------------------------------------------------------------
 
 def test_binding_refuses_host_tensors_and_types():
