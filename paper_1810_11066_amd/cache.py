@@ -339,14 +339,14 @@ def attend(q: torch.Tensor, cache, table: torch.Tensor, lengths: torch.Tensor,
     if rows != batch or _int32(lengths, "lengths", 1, device)[0] != batch:
         raise ValueError("%d queries, %d rows of the table and %d lengths"
                          % (batch, rows, lengths.shape[0]))
-    if max_len is None:
-        max_len = max_pages * page_tokens
-    need = _workspace(device, cache[0].shape[0], kv_heads, page_tokens, dim,
-                      batch, heads, max_pages, max_len, window, kind)
     out = torch.empty_like(q, memory_format=torch.contiguous_format)
     lse = torch.empty(batch, heads, dtype=torch.float32, device=q.device)
     if batch == 0:
         return out, lse
+    if max_len is None:
+        max_len = max_pages * page_tokens
+    need = _workspace(device, cache[0].shape[0], kv_heads, page_tokens, dim,
+                      batch, heads, max_pages, max_len, window, kind)
     space = torch.empty(need, dtype=torch.uint8, device=q.device) if need \
         else None
     _call(device, (_lib or load_library()).bscache_attend, pages,

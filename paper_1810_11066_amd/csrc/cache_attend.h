@@ -114,13 +114,34 @@ __device__ __forceinline__ int32_t places_of(const Attend& a, int32_t b,
     return b < a.batch ? pair_places(span_of(a, length).units()) : 0;
 }
 
-// Places of the sequences from 64 on.
-__device__ __forceinline__ int32_t places_behind(const Attend& a, int lane) {
-    int32_t total = 0;
-    for (int32_t b = 64; b < a.batch; b += 64)
-        total += __builtin_amdgcn_readlane(
-            wave_scan(places_of(a, b + lane, length_of(a, b + lane))), 63);
-    return total;
+// All sequences' places, for one head tile, over the lanes of a wave: lane l has
+// the `per` sequences from l per on, so that a batch of any size takes two
+// rounds of loads, this one and that over one lane's sequences.
+struct Row {
+    int32_t per;              // sequences of a lane
+    int32_t length;           // the lane's first sequence's
+    int32_t mine, sum;        // the lane's places, and with the lanes' before
+    int32_t total;
+};
+__device__ __forceinline__ Row all_places(const Attend& a, int lane) {
+    constexpr int kDeep = 8;  // loads in flight
+    Row r;
+    r.per = (a.batch + 63) >> 6;
+    r.length = length_of(a, lane * r.per);
+    r.mine = places_of(a, lane * r.per, r.length);
+    for (int32_t k = 1; k < r.per; k += kDeep) {
+        int32_t length[kDeep];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+            length[u] = length_of(a, lane * r.per + min(k + u, r.per - 1));
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+            if (k + u < r.per)
+                r.mine += places_of(a, lane * r.per + k + u, length[u]);
+    }
+    r.sum = wave_scan(r.mine);
+    r.total = __builtin_amdgcn_readlane(r.sum, 63);
+    return r;
 }
 
 // A word of a table that the kernel only reads, at a place that is the same
@@ -352,35 +373,37 @@ void attend_kernel(const Attend a) {
         lengths = uniform_load(a.lengths, seq);
         lengths_of = seq;
     } else {
-        lengths = length_of(a, lane);
-        int32_t own = places_of(a, lane, lengths);
-        int32_t sum = wave_scan(own);
-        const int32_t total = (__builtin_amdgcn_readlane(sum, 63) +
-                               places_behind(a, lane)) * pairs;
+        const Row r = all_places(a, lane);
+        const int32_t total = r.total * pairs;
         const int32_t sharers = sharing(a, total);
         if (self >= sharers) return;
         place = range_start(self, total, sharers);
         place_end = range_start(self + 1, total, sharers);
-        int32_t before = 0;          // places before seq, for one head tile
-        for (int32_t b = 0;;) {
-            const int32_t all = __builtin_amdgcn_readlane(sum, 63);
-            if (place < (before + all) * pairs) {
-                const uint64_t past = __ballot((before + sum) * pairs > place);
-                const int at = __builtin_ctzll(past);
-                const int32_t its = __builtin_amdgcn_readlane(own, at);
-                seq = b + at;
-                before += __builtin_amdgcn_readlane(sum, at) - its;
-                pair = (place - before * pairs) / its;
-                pair_start = before * pairs + pair * its;
-                break;
+        // the lane whose sequences hold the first place, then the sequence
+        int at = __builtin_ctzll(__ballot(r.sum * pairs > place));
+        int32_t before = __builtin_amdgcn_readlane(r.sum - r.mine, at);
+        int32_t own = r.mine, sum = r.sum;
+        lengths = r.length;
+        if (r.per > 1) {
+            lengths_of = at * r.per;
+            for (;;) {
+                lengths = length_of(a, lengths_of + lane);
+                own = places_of(a, lengths_of + lane, lengths);
+                sum = before + wave_scan(own);
+                const uint64_t past = __ballot(sum * pairs > place);
+                if (past) {
+                    at = __builtin_ctzll(past);
+                    break;
+                }
+                before = __builtin_amdgcn_readlane(sum, 63);
+                lengths_of += 64;
             }
-            before += all;
-            b += 64;
-            lengths_of = b;
-            lengths = length_of(a, b + lane);
-            own = places_of(a, b + lane, lengths);
-            sum = wave_scan(own);
         }
+        const int32_t its = __builtin_amdgcn_readlane(own, at);
+        seq = lengths_of + at;
+        before = __builtin_amdgcn_readlane(sum, at) - its;
+        pair = (place - before * pairs) / its;
+        pair_start = before * pairs + pair * its;
     }
 
     for (bool again = false;;) {

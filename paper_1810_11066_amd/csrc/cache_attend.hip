@@ -33,21 +33,17 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a,
     const int64_t row0 =
         (int64_t)seq * a.heads + kvh * a.group + tile16 * 16 + h0;
 
-    int32_t total = 0, start = 0, length = 0;
-    for (int32_t b = 0; b < a.batch; b += 64) {
-        const int32_t its = length_of(a, b + lane);
-        const int32_t own = places_of(a, b + lane, its);
-        const int32_t sum = wave_scan(own);
-        if (seq >= b && seq < b + 64) {
-            const int32_t places = __builtin_amdgcn_readlane(own, seq - b);
-            length = __builtin_amdgcn_readlane(its, seq - b);
-            start = (total + __builtin_amdgcn_readlane(sum, seq - b) - places) *
-                        pairs + pair * places;
-        }
-        total += __builtin_amdgcn_readlane(sum, 63);
+    const Row r0 = all_places(a, lane);
+    const int32_t total = r0.total * pairs;
+    const int32_t units = span_of(a, uniform_load(a.lengths, seq)).units();
+    const int lane0 = seq / r0.per;
+    int32_t before = __builtin_amdgcn_readlane(r0.sum - r0.mine, lane0);
+    for (int32_t b = lane0 * r0.per; b < seq; b += 64) {
+        const int32_t own = places_of(a, b + lane, length_of(a, b + lane));
+        before += __builtin_amdgcn_readlane(
+            wave_scan(b + lane < seq ? own : 0), 63);
     }
-    total *= pairs;
-    const int32_t units = span_of(a, length).units();
+    const int32_t start = before * pairs + pair * pair_places(units);
     const int32_t sharers = sharing(a, total);
     const int32_t i0 = range_of(start, total, sharers);
     const int32_t parts =

@@ -294,14 +294,18 @@ def test_attend_split_sequences(kind, batch, longest):
             kind=kind)
 
 
-def test_attend_many_sequences():
-    """More sequences than lanes of a wave, most of them short."""
-    rng = np.random.default_rng(3)
-    batch = 300
+@pytest.mark.parametrize("batch", [64, 65, 300, 4096, 4500])
+def test_attend_many_sequences(batch):
+    """More sequences than lanes of a wave, more than 64 for a lane; most of
+    them short, some empty, one long enough for every way to be shared."""
+    rng = np.random.default_rng(batch)
     lengths = rng.choice([0, 1, 7, 40, 200], batch)
+    lengths[batch - 2] = 2600
     f = Filled(rng, 30, 1, 16, 16, 4, 4)
-    table = rng.integers(0, 30, (batch, 13)).astype(np.int32)
-    f.check(queries(rng, batch, 2, 16, "f16"), torch.from_numpy(table).cuda(),
+    table = rng.integers(0, 30, (batch, 163)).astype(np.int32)
+    assert " shared " in kc.describe(30, 1, 16, 16, batch, 1, 163 * 16, 4, 4,
+                                     dtype=torch.float16)
+    f.check(queries(rng, batch, 1, 16, "f16"), torch.from_numpy(table).cuda(),
             torch.tensor(lengths, dtype=torch.int32, device="cuda"),
             kind="f16")
 
@@ -413,7 +417,7 @@ def test_no_work_is_valid():
     k, v = kc.read(none, f.cache, 64)
     assert k.shape == v.shape == (0, 1, 64)
     out, lse = kc.attend(empty, f.cache,
-                         torch.empty((0, 2), dtype=torch.int32,
+                         torch.empty((0, 0), dtype=torch.int32,
                                      device="cuda"), none)
     assert out.shape == (0, 1, 64) and lse.shape == (0, 1)
 
