@@ -604,8 +604,7 @@ static bscache_status check_attend(const bscache_pages* cache,
         return fail(BSCACHE_ERR_UNSUPPORTED,
                     "more than 2^31 - 1 tiles of 64 tokens, or rows");
     bscache::plan_attend(*a, span);
-    *workspace =
-        a->whole ? 0 : (int64_t)a->blocks * 2 * 16 * (a->c.dim + 2) * 4;
+    *workspace = a->workspace;
     return BSCACHE_OK;
 }
 

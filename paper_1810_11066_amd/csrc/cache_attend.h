@@ -104,14 +104,16 @@ __device__ __forceinline__ int32_t wave_scan(int32_t v) {
 }
 
 // Places of a pair in the row: its units, then an empty one, or as many as make
-// four, for what it costs to begin and end a pair.
-__device__ __forceinline__ int32_t pair_places(int32_t units) {
-    return units + 1 > 4 ? units + 1 : 4;
+// `least`, for what it costs to begin and end a pair: 4.6 us, against 1.3 us a
+// unit where a workgroup has one or two pairs, and 2.6 us where it has many and
+// the memory is busy.
+__device__ __forceinline__ int32_t pair_places(const Attend& a, int32_t units) {
+    return max(units + 1, a.least);
 }
 // Those of sequence b, for one head tile.
 __device__ __forceinline__ int32_t places_of(const Attend& a, int32_t b,
                                              int32_t length) {
-    return b < a.batch ? pair_places(span_of(a, length).units()) : 0;
+    return b < a.batch ? pair_places(a, span_of(a, length).units()) : 0;
 }
 
 // All sequences' places, for one head tile, over the lanes of a wave: lane l has
@@ -159,14 +161,17 @@ __device__ __forceinline__ int32_t sharing(const Attend& a, int32_t u) {
 __device__ __forceinline__ int32_t range_start(int32_t i, int32_t u, int32_t n) {
     return (int32_t)((int64_t)u * i / n);
 }
-// The workgroup whose range holds place x.
-__device__ __forceinline__ int32_t range_of(int32_t x, int32_t u, int32_t n) {
-    return (int32_t)((((int64_t)x + 1) * n - 1) / u);
-}
-
 // Partial results: slot 2 i of workgroup i for the pair that began before its
 // range, 2 i + 1 for the pair that goes on behind it.  A slot holds [16][dim]
 // sums and [16][2] maximum (of mo, see below) and sum of weights.
+// Behind the slots, for every pair: the workgroups of its first and last units.
+__host__ __device__ __forceinline__ int64_t part_bytes(int32_t dim) {
+    return 64 * (dim + 2);
+}
+__device__ __forceinline__ int32_t* ends_of(const Attend& a) {
+    return reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(a.parts) +
+                                      2 * a.blocks * part_bytes(a.c.dim));
+}
 __device__ __forceinline__ float* part_of(const Attend& a, int32_t slot) {
     return a.parts + (int64_t)slot * 16 * (a.c.dim + 2);
 }
@@ -419,7 +424,14 @@ void attend_kernel(const Attend a) {
         if (!one) {
             c0 = min(place - pair_start, units);
             c1 = min(place_end - pair_start, units);
-            pair_start += pair_places(units);
+            if (c0 < c1 && wave == 0 && lane == 0) {
+                // for the join: the first and the last workgroup of the pair
+                int32_t* ends = ends_of(a) + 2 * ((int64_t)seq * pairs + pair);
+                const int me = here(self);
+                if (c0 == 0) ends[0] = me;
+                if (c1 == units) ends[1] = me;
+            }
+            pair_start += pair_places(a, units);
             place = pair_start;
         }
         const int32_t kvh = pair / a.head_tiles;

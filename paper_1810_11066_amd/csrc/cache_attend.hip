@@ -13,14 +13,13 @@ namespace {
 // partial results each.  Threads are columns of 4 channels of a head, times
 // rows that take every rows-th partial result and are added at the end; a
 // thread has kDeep of them in flight, and a running maximum of its own, so
-// that no load waits for another but the lengths'.
+// that no load waits for another but the pair's entry.
 constexpr int kDeep = 8, kThreads = 256;
 
 __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a,
                                                         int32_t few) {
     __shared__ f32x4 sm_r[kThreads];
     __shared__ float2 sm_ml[kThreads];
-    const int lane = threadIdx.x & 63;
     const int dim = a.c.dim, quads = dim >> 2;
     const int32_t pairs = a.c.kv_heads * a.head_tiles;
     const int32_t slices = (min(a.group, 16) + few - 1) / few;
@@ -33,21 +32,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a,
     const int64_t row0 =
         (int64_t)seq * a.heads + kvh * a.group + tile16 * 16 + h0;
 
-    const Row r0 = all_places(a, lane);
-    const int32_t total = r0.total * pairs;
-    const int32_t units = span_of(a, uniform_load(a.lengths, seq)).units();
-    const int lane0 = seq / r0.per;
-    int32_t before = __builtin_amdgcn_readlane(r0.sum - r0.mine, lane0);
-    for (int32_t b = lane0 * r0.per; b < seq; b += 64) {
-        const int32_t own = places_of(a, b + lane, length_of(a, b + lane));
-        before += __builtin_amdgcn_readlane(
-            wave_scan(b + lane < seq ? own : 0), 63);
-    }
-    const int32_t start = before * pairs + pair * pair_places(units);
-    const int32_t sharers = sharing(a, total);
-    const int32_t i0 = range_of(start, total, sharers);
-    const int32_t parts =
-        range_of(start + units - 1, total, sharers) - i0 + 1;
+    const int2 ends = *reinterpret_cast<const int2*>(ends_of(a) + 2 * at);
+    const int32_t i0 = ends.x, parts = ends.y - i0 + 1;
     if (parts == 1) return;          // its workgroup wrote the output
 
     const int32_t columns = heads * quads;
@@ -148,6 +134,9 @@ void plan_attend(Attend& a, int64_t tokens) {
               (units <= 16 && 2 * pairs >= at_once);
     const int64_t n = a.whole ? pairs : std::min(pairs * units, at_once);
     a.blocks = (int32_t)std::max(n, (int64_t)1);
+    a.least = pairs >= 4 * n ? 2 : 3;
+    const int64_t parts = 2 * a.blocks * part_bytes(a.c.dim);
+    a.workspace = a.whole ? 0 : parts + 8 * pairs;
 }
 
 hipError_t launch_attend(const Attend& a, hipStream_t st) {

@@ -204,7 +204,9 @@ def plan(batch, max_len, kv_heads=8, dim=128, group=4, **kw):
 def test_plan_rules(batch, max_len, way, grid, waves):
     w, g, n, space = plan(batch, max_len)
     assert (w, g, n) == (way, grid, waves)
-    assert space == (grid * 2 * 16 * (128 + 2) * 4 if way == "shared" else 0)
+    # two partial results of 16 heads a workgroup, an entry for every pair
+    assert space == (grid * 2 * 16 * (128 + 2) * 4 + 8 * 8 * batch
+                     if way == "shared" else 0)
 
 
 def test_plan_follows_registers_window_and_head_tiles():
