@@ -126,7 +126,7 @@ bscache_status bscache_read(const bscache_pages *cache, const int32_t *slots,
  *            table[b][t / page_tokens]; entries behind its last page are not
  *            used.  Tokens of an entry outside the cache are not visible;
  *   lengths: [batch] int32; one above max_len counts as max_len, one below 0
- *            as 0;
+ *            as 0; they must not change while the call runs;
  *   out:     [batch][heads][dim] of type dtype;
  *   lse:     [batch][heads] float32, or NULL.
  * A sequence without a visible token gets out = 0 and lse = -inf.  A query
@@ -134,7 +134,8 @@ bscache_status bscache_read(const bscache_pages *cache, const int32_t *slots,
  * Products are of the exact codes: q enters the matrix units scaled by a power
  * of two as float16 (bfloat16 and float16 values keep their bits but for what
  * lies below 2^-30 of the row's largest; float32 as two float16 of 22 bits
- * together), weights times s as float16 (float32 calls: two); sums and the softmax are binary32.
+ * together), weights times s as float16 (float16 and float32 calls: two);
+ * sums and the softmax are binary32.
  * The workspace holds partial results of sequences that several workgroups
  * share: bscache_attend_workspace() bytes (0 for short max_len), 16-byte
  * aligned, contents irrelevant before and after.

@@ -54,7 +54,9 @@
 // go past the L2s of the XCDs, and a call of few pairs and many partial
 // results leaves them to one workgroup; 1 us shorter with up to 8 of them a
 // pair, 9 to 16 us longer with 64 and more.)  Calls of short sequences
-// (Attend::whole) give every pair to one workgroup instead.
+// (Attend::whole) give every pair to one workgroup instead.  Lengths that change
+// during a call make its results wrong, but the number of the sequence, of the
+// loops' rounds and of the partial results stays within the call's.
 #pragma once
 
 #include "cache_internal.h"
@@ -103,17 +105,17 @@ __device__ __forceinline__ int32_t wave_scan(int32_t v) {
     return scan_step<0x143, 0xC>(v);    // row_bcast 31 into rows 2 and 3
 }
 
-// Places of a pair in the row: its units, then an empty one, or as many as make
-// `least`, for what it costs to begin and end a pair: 4.6 us, against 1.3 us a
-// unit where a workgroup has one or two pairs, and 2.6 us where it has many and
-// the memory is busy.
-__device__ __forceinline__ int32_t pair_places(const Attend& a, int32_t units) {
-    return max(units + 1, a.least);
+// Places of a pair in the row: its units, then an empty one for what it costs to
+// begin and end a pair (4.6 us, against 1.3 us a unit where a workgroup has one
+// or two pairs, and 2.6 us where it has many and the memory is busy; at least 3
+// places a pair: 1000 sequences of 1-4096 tokens 284 us for 272).
+__device__ __forceinline__ int32_t pair_places(int32_t units) {
+    return units + 1;
 }
 // Those of sequence b, for one head tile.
 __device__ __forceinline__ int32_t places_of(const Attend& a, int32_t b,
                                              int32_t length) {
-    return b < a.batch ? pair_places(a, span_of(a, length).units()) : 0;
+    return b < a.batch ? pair_places(span_of(a, length).units()) : 0;
 }
 
 // All sequences' places, for one head tile, over the lanes of a wave: lane l has
@@ -402,6 +404,7 @@ void attend_kernel(const Attend a) {
                 }
                 before = __builtin_amdgcn_readlane(sum, 63);
                 lengths_of += 64;
+                if (lengths_of >= a.batch) return;   // (see above)
             }
         }
         const int32_t its = __builtin_amdgcn_readlane(own, at);
@@ -431,7 +434,7 @@ void attend_kernel(const Attend a) {
                 if (c0 == 0) ends[0] = me;
                 if (c1 == units) ends[1] = me;
             }
-            pair_start += pair_places(a, units);
+            pair_start += pair_places(units);
             place = pair_start;
         }
         const int32_t kvh = pair / a.head_tiles;
@@ -441,7 +444,7 @@ void attend_kernel(const Attend a) {
             pair = 0;
             ++seq;
         }
-        const bool last = one || place >= place_end;
+        const bool last = one || place >= place_end || seq >= a.batch;
         if (c0 >= c1) {              // nothing but empty places
             if (last) break;
             continue;
@@ -739,7 +742,7 @@ void attend_kernel(const Attend a) {
             }
         }
 
-        // ---- the four waves' results
+        // ---- the waves' results
         sum_p = over_groups(sum_p, add);
         sum_z = over_groups(sum_z, add);
         const int end_lane = here(lane);

@@ -33,8 +33,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a,
         (int64_t)seq * a.heads + kvh * a.group + tile16 * 16 + h0;
 
     const int2 ends = *reinterpret_cast<const int2*>(ends_of(a) + 2 * at);
-    const int32_t i0 = ends.x, parts = ends.y - i0 + 1;
-    if (parts == 1) return;          // its workgroup wrote the output
+    const int32_t i0 = max(ends.x, 0);
+    const int32_t parts = min(ends.y, a.blocks - 1) - i0 + 1;
+    if (parts <= 1) return;          // its workgroup wrote the output
 
     const int32_t columns = heads * quads;
     const int32_t rows = columns < kThreads ? kThreads / max(columns, 1) : 1;
@@ -134,7 +135,6 @@ void plan_attend(Attend& a, int64_t tokens) {
               (units <= 16 && 2 * pairs >= at_once);
     const int64_t n = a.whole ? pairs : std::min(pairs * units, at_once);
     a.blocks = (int32_t)std::max(n, (int64_t)1);
-    a.least = pairs >= 4 * n ? 2 : 3;
     const int64_t parts = 2 * a.blocks * part_bytes(a.c.dim);
     a.workspace = a.whole ? 0 : parts + 8 * pairs;
 }

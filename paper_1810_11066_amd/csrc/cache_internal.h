@@ -144,7 +144,6 @@ struct Attend {
     bool whole;               // every pair is one workgroup's
     bool wide;                // of as many waves as a CU holds (whole too)
     int32_t blocks;           // workgroups
-    int32_t least;            // fewest places of a pair
     int64_t workspace;        // bytes
 };
 
