@@ -99,6 +99,16 @@ def load_library():
         return lib
 
 
+def _params(*values) -> bytes:
+    """Packed bscache_attend_params."""
+    try:
+        return _PARAMS.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise ValueError("batch, heads, max_pages, max_len and window must be "
+                         "32-bit integers, scale a binary32 number (got %s)"
+                         % (values[1:6] + values[7:],)) from e
+
+
 def _check(status: int):
     if status != OK:
         raise CacheError(status, load_library().bscache_last_error().decode())
@@ -237,8 +247,8 @@ def _workspace(device: int, pages: int, kv_heads: int, page_tokens: int,
     the device's compute units."""
     need = ctypes.c_int64()
     cache = _PAGES.pack(pages, kv_heads, page_tokens, dim, 8, 8, 0, 0, 0, 0)
-    params = _PARAMS.pack(heads * dim, batch, heads, max_pages, max_len,
-                          window, dtype, 1.0)
+    params = _params(heads * dim, batch, heads, max_pages, max_len, window,
+                     dtype, 1.0)
     _call(device, load_library().bscache_attend_workspace, cache, params,
           ctypes.byref(need))
     return need.value
@@ -350,8 +360,8 @@ def attend(q: torch.Tensor, cache, table: torch.Tensor, lengths: torch.Tensor,
     space = torch.empty(need, dtype=torch.uint8, device=q.device) if need \
         else None
     _call(device, (_lib or load_library()).bscache_attend, pages,
-          _PARAMS.pack(q_stride, batch, heads, max_pages, max_len, window,
-                       kind, dim ** -0.5 if scale is None else scale),
+          _params(q_stride, batch, heads, max_pages, max_len, window, kind,
+                  dim ** -0.5 if scale is None else scale),
           q.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(),
           lse.data_ptr(), space.data_ptr() if need else None, need,
           _stream(device))
@@ -366,6 +376,6 @@ def describe(pages: int, kv_heads: int, page_tokens: int, dim: int,
     _check(load_library().bscache_attend_describe(
         _PAGES.pack(pages, kv_heads, page_tokens, dim, kbits, vbits, 0, 0, 0,
                     0),
-        _PARAMS.pack(heads * dim, batch, heads, -(-max_len // page_tokens),
-                     max_len, window, _DTYPES[dtype], 1.0), buf, 256))
+        _params(heads * dim, batch, heads, -(-max_len // page_tokens), max_len,
+                window, _DTYPES[dtype], 1.0), buf, 256))
     return buf.value.decode()

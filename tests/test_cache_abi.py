@@ -370,3 +370,9 @@ def test_reference_attention_is_the_softmax():
     assert np.allclose(out, want.numpy() @ v, rtol=1e-12, atol=1e-12)
     assert abs(lse - np.log(np.exp(k @ q * 0.25).sum())) < 1e-12
     assert (tol > 0).all() and (tol < 1e-4).all()
+
+
+def test_binding_refuses_numbers_that_no_field_holds():
+    for kw in ({"window": 1 << 40}, {"max_len": 1 << 31}, {"window": 1.5}):
+        with pytest.raises(ValueError, match="32-bit"):
+            kc.describe(4, 1, 16, 64, 1, 4, **{"max_len": 16, **kw})
