@@ -96,26 +96,27 @@ __device__ __forceinline__ uint32_t nibbles(uint32_t d) {
     return (d | d >> 8) & 0xFFFFu;
 }
 
-// the four nibbles of 2 bytes as 4 bytes
+// the four nibbles of the low 2 bytes as 4 bytes
 __device__ __forceinline__ uint32_t spread(uint32_t w) {
-    w = (w | w << 8) & 0x00FF00FFu;
+    w = (w & 0xFFu) | (w & 0xFF00u) << 8;
     return (w | w << 4) & 0x0F0F0F0Fu;
 }
 
 // Values read back go past the caches (non-temporal stores): they push out
-// nothing that is read sooner, and are not fetched before they are written
-// (100000 tokens of 8 heads of 128 in 123.4 us, 131.3 without).
+// nothing that is read sooner (16384 tokens of 8 heads of 128 in 17.1
+// us, 24.4 without; 100000 in 108.7 and 117.6).
 template <class V>
 __device__ __forceinline__ void stream(V* p, V v) {
     __builtin_nontemporal_store(v, p);
 }
 
 // Bound by memory, and next by the vector ALUs (about 130 instructions for 8
-// channels a lane: 16 bytes of float16).  Codes are stored the ordinary way:
-// past the caches a large write by itself takes 2 to 4 us less (21 us for
-// 16384 tokens of 8 heads of 128), but the read or the attention that comes
-// next finds them in the caches (write and read of 16384 tokens together
-// 38.2 us, 44.9 past the caches; of 60000 tokens of 2 heads 35.0 and 40.1).
+// channels a lane: 16 bytes of float16): 100000 tokens of 8 heads of 128, 570
+// MB, in 114.6 us = 5.0 TB/s.  Codes are stored the ordinary way: past the
+// caches a write by itself takes 0 to 5 us less (60000 tokens of 8 heads of 64
+// 37.2 for 41.4 us), but the read or the attention that comes next finds them in
+// the caches (write and read of those together 66.6 us, 75.8 past the caches; of
+// 16384 tokens of 4-bit codes, 128 channels 34.6 and 39.8).
 template <int T, int LPR, int STEPS>
 __global__ __launch_bounds__(kBlock) void write_kernel(
     Pages c, const void* __restrict__ k, const void* __restrict__ v,
@@ -183,6 +184,10 @@ __global__ __launch_bounds__(kBlock) void write_kernel(
     }
 }
 
+// Bound by memory: 100000 tokens of 8 heads of 128, 570 MB, in 108 us = 5.3 TB/s,
+// what a copy reaches.  (Nothing looks at a code before all of a wave's loads are
+// sent: 4-bit ones spread where they are loaded took 121 us.)
+//
 // A lane's codes are two times 4 channels: next to each other where the values
 // are written as one 16-byte store of 16 bits each, LPR lanes apart where they
 // are float32, so that a store of 4 of them leaves no gap between the lanes.
@@ -199,17 +204,20 @@ __global__ __launch_bounds__(kBlock) void read_kernel(
     const int channel = lane % LPR * (T == kF32 ? 4 : 8);
     const int bits = c.bits[side];
     const uint8_t* codes = c.codes[side];
-    uint32_t d[STEPS][2], sz[STEPS];
+    uint32_t slot[STEPS], d[STEPS][2], sz[STEPS];
     const int64_t t0 = first + lane / LPR;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
         const int64_t t = t0 + s * kRows;
-        const uint32_t slot = t < g.tokens ? (uint32_t)slots[t] : ~0u;
+        slot[s] = t < g.tokens ? (uint32_t)slots[t] : ~0u;
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
         d[s][0] = d[s][1] = sz[s] = 0;     // a slot outside the cache: 0 + 0 c
-        if (slot < c.slots && channel < c.dim) {
-            const uint32_t page = c.by_page.div(slot);
+        if (slot[s] < c.slots && channel < c.dim) {
+            const uint32_t page = c.by_page.div(slot[s]);
             const int64_t row = row_of(c, page, head,
-                                       slot - page * c.by_page.d);
+                                       slot[s] - page * c.by_page.d);
             sz[s] = c.steps[side][row];
             const uint8_t* p = codes + row * (c.dim * bits >> 3) +
                                (channel * bits >> 3);
@@ -220,17 +228,16 @@ __global__ __launch_bounds__(kBlock) void read_kernel(
                     if (both)
                         d[s][1] = *reinterpret_cast<const uint32_t*>(p + kApart);
                 } else {
-                    d[s][0] = spread(*reinterpret_cast<const uint16_t*>(p));
+                    d[s][0] = *reinterpret_cast<const uint16_t*>(p);
                     if (both)
-                        d[s][1] = spread(
-                            *reinterpret_cast<const uint16_t*>(p + kApart / 2));
+                        d[s][1] =
+                            *reinterpret_cast<const uint16_t*>(p + kApart / 2);
                 }
             } else if (bits == 8) {
                 const u32x2 w = *reinterpret_cast<const u32x2*>(p);
                 d[s][0] = w[0], d[s][1] = w[1];
             } else {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
-                d[s][0] = spread(w & 0xFFFFu), d[s][1] = spread(w >> 16);
+                d[s][0] = *reinterpret_cast<const uint32_t*>(p);
             }
         }
     }
@@ -240,6 +247,11 @@ __global__ __launch_bounds__(kBlock) void read_kernel(
     for (int s = 0; s < STEPS; ++s, at += (int64_t)kRows * c.kv_heads * c.dim) {
         if (t0 + s * kRows >= g.tokens || channel >= c.dim) continue;
         const float step = step_of(sz[s]), z = offset_of(sz[s]);
+        if (bits == 4) {    // (not sooner: it waits for the codes)
+            if constexpr (T != kF32) d[s][1] = d[s][0] >> 16;
+            d[s][0] = spread(d[s][0]);
+            d[s][1] = spread(d[s][1]);
+        }
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -266,7 +278,7 @@ __global__ __launch_bounds__(kBlock) void read_kernel(
 // fn<T, LPR, STEPS>(args) for the run-time type, row width and stretch.
 template <template <int, int, int> class F, int T, int LPR, class... A>
 hipError_t pick_steps(int steps, A... a) {
-    return steps == 4 ? F<T, LPR, 4>::go(a...) : F<T, LPR, 1>::go(a...);
+    return steps == 2 ? F<T, LPR, 2>::go(a...) : F<T, LPR, 1>::go(a...);
 }
 template <template <int, int, int> class F, int T, class... A>
 hipError_t pick_lpr(int lpr, int steps, A... a) {
@@ -305,15 +317,16 @@ struct Read {
     }
 };
 
-// Lanes of a row, stretches and grid of a call.
-RowsGrid rows_grid(const Pages& c, int64_t tokens, int* lpr, int* steps) {
+// Lanes of a row, groups of a wave and grid of a call: two groups once the waves
+// of single ones are more than `full` on a SIMD.
+RowsGrid rows_grid(const Pages& c, int64_t tokens, int full, int* lpr,
+                   int* steps) {
     *lpr = 2;
     while (*lpr * 8 < c.dim) *lpr *= 2;
     const int rows = 64 / *lpr;
     const int64_t pairs = 2 * (int64_t)c.kv_heads;
-    // stretches of 4 once the waves of single ones are 8 on a SIMD
-    *steps = (tokens + rows - 1) / rows * pairs >=
-                     (int64_t)device_cus() * 4 * 8 ? 4 : 1;
+    *steps = (tokens + rows - 1) / rows * pairs >
+                     (int64_t)device_cus() * 4 * full ? 2 : 1;
     RowsGrid g;
     g.tokens = tokens;
     g.groups = (uint32_t)((tokens + rows * *steps - 1) / (rows * *steps));
@@ -345,7 +358,9 @@ hipError_t launch_write(const Pages& c, const void* k, const void* v,
                         const int32_t* slots, int64_t tokens,
                         hipStream_t st) {
     int lpr, steps;
-    const RowsGrid g = rows_grid(c, tokens, &lpr, &steps);
+    // (8192 tokens, 32 waves a SIMD: 11.9 us single, 12.5 in twos; 16384: 22.0
+    // and 20.5; in fours 13.1 and 21.0)
+    const RowsGrid g = rows_grid(c, tokens, 32, &lpr, &steps);
     return pick<Write>(dtype, lpr, steps, c, k, v, k_stride, v_stride, slots,
                        g, st);
 }
@@ -353,7 +368,9 @@ hipError_t launch_write(const Pages& c, const void* k, const void* v,
 hipError_t launch_read(const Pages& c, const int32_t* slots, int64_t tokens,
                        void* k, void* v, int dtype, hipStream_t st) {
     int lpr, steps;
-    const RowsGrid g = rows_grid(c, tokens, &lpr, &steps);
+    // (1024 tokens of 8 heads of 128, 4 waves a SIMD: 3.3 us single, 3.4 in
+    // twos; 2048: 4.2 and 3.9; 100000: 137 and 108; in fours 3.8, 4.1 and 107)
+    const RowsGrid g = rows_grid(c, tokens, 7, &lpr, &steps);
     return pick<Read>(dtype, lpr, steps, c, slots, k, v, g, st);
 }
 
