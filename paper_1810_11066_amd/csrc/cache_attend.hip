@@ -8,20 +8,20 @@ namespace bscache {
 namespace {
 
 // Adds the partial results of a pair that several workgroups share, in their
-// order.  A workgroup of this kernel takes `few` query heads of one pair: all
-// of its tile where pairs are many, one where pairs are few and have many
-// partial results each.  Threads are columns of 4 channels of a head, times
-// rows that take every rows-th partial result and are added at the end; a
-// thread has kDeep of them in flight, and a running maximum of its own, so
-// that no load waits for another but the pair's entry.
+// order.  A workgroup of this kernel takes a.few query heads of one pair.
+// Threads are columns of 4 channels of a head, times rows that take every
+// rows-th partial result and are added at the end; a thread has kDeep of them
+// in flight, and a running maximum of its own, so that no load waits for
+// another but the pair's entry.  4 to 5 us, most of it the launch and two
+// loads after one another.
 constexpr int kDeep = 8, kThreads = 256;
 
-__global__ __launch_bounds__(kThreads) void join_kernel(const Attend a,
-                                                        int32_t few) {
+__global__ __launch_bounds__(kThreads) void join_kernel(const Attend a) {
     __shared__ f32x4 sm_r[kThreads];
     __shared__ float2 sm_ml[kThreads];
     const int dim = a.c.dim, quads = dim >> 2;
     const int32_t pairs = a.c.kv_heads * a.head_tiles;
+    const int32_t few = a.few;
     const int32_t slices = (min(a.group, 16) + few - 1) / few;
     const int32_t at = blockIdx.x / slices;
     const int32_t seq = at / pairs, pair = at - seq * pairs;
@@ -122,7 +122,11 @@ template <> hipError_t launch_attend_dp<256>(const Attend&, hipStream_t);
 //
 // Everything else is shared: as many workgroups as run at once, each with its
 // part (4 times as many, taken up as others end: 551 us for 524 at 128
-// sequences of 12-16 Ki tokens).
+// sequences of 12-16 Ki tokens).  The join takes all heads of a tile together
+// where pairs are many (64 ragged sequences 28.6 us, 30.5 head by head), and
+// where one round of loads does for as many partial results as a sequence may
+// have (16 x 2048 tokens 20.2 and 20.8); otherwise it takes them one by one (1 x
+// 8192 tokens 12.8 us, 14.6 together; 256 channels 29.2 and 36.1).
 void plan_attend(Attend& a, int64_t tokens) {
     const int64_t pairs = (int64_t)a.batch * a.c.kv_heads * a.head_tiles;
     const int dp = padded_dim(a.c.dim);
@@ -135,6 +139,9 @@ void plan_attend(Attend& a, int64_t tokens) {
               (units <= 16 && 2 * pairs >= at_once);
     const int64_t n = a.whole ? pairs : std::min(pairs * units, at_once);
     a.blocks = (int32_t)std::max(n, (int64_t)1);
+    const int heads = std::min(a.group, 16);
+    a.few = pairs >= cus || heads * (a.c.dim >> 2) * units <= kDeep * kThreads
+                ? heads : 1;
     const int64_t parts = 2 * a.blocks * part_bytes(a.c.dim);
     a.workspace = a.whole ? 0 : parts + 8 * pairs;
 }
@@ -146,10 +153,8 @@ hipError_t launch_attend(const Attend& a, hipStream_t st) {
                                      : launch_attend_dp<64>(a, st);
     if (e != hipSuccess || a.whole) return e;
     const int32_t pairs = a.batch * a.c.kv_heads * a.head_tiles;
-    const int32_t heads = std::min(a.group, 16);
-    const int32_t few = pairs < device_cus() ? 1 : heads;
-    return launch(join_kernel, pairs * ((heads + few - 1) / few), kThreads, st,
-                  a, few);
+    const int32_t slices = (std::min(a.group, 16) + a.few - 1) / a.few;
+    return launch(join_kernel, pairs * slices, kThreads, st, a);
 }
 
 }  // namespace bscache

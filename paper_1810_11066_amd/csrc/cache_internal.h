@@ -144,6 +144,7 @@ struct Attend {
     bool whole;               // every pair is one workgroup's
     bool wide;                // of as many waves as a CU holds (whole too)
     int32_t blocks;           // workgroups
+    int32_t few;              // query heads of a workgroup of the join
     int64_t workspace;        // bytes
 };
 
@@ -166,8 +167,8 @@ constexpr int group_waves(int dp, int dtype, bool wide) {
 // Tokens of a unit: what the 4 waves of a workgroup take in one step.
 constexpr int kUnit = 128;
 
-// Chooses `whole`, `wide` and `blocks` for a call whose longest sequence spans
-// `tokens` tokens.
+// Chooses `whole`, `wide`, `blocks`, `few` and the workspace for a call whose
+// longest sequence spans `tokens` tokens.
 void plan_attend(Attend& a, int64_t tokens);
 
 hipError_t launch_attend(const Attend& a, hipStream_t st);
