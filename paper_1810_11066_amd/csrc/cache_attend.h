@@ -335,6 +335,15 @@ __device__ __forceinline__ int here(int x) {
     return x;
 }
 
+// x with all its bits as they are here.  A product that is rounded to float16 may
+// be computed a second time for that, with one rounding instead of two
+// (v_fma_mixlo_f16, whatever -ffp-contract says): next to a tie the two differ
+// by a step of float16, and a rest taken from the other one misses it.
+__device__ __forceinline__ float rounded(float x) {
+    asm("" : "+v"(x));
+    return x;
+}
+
 // Where the two halves of a wave's tile lie: the row of each half's first
 // token, and the end of its visible tokens (0 where its page is none of the
 // cache).  Half a tile never leaves a page (pages are multiples of 16 tokens).
@@ -575,6 +584,7 @@ void attend_kernel(const Attend a) {
             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
+                    // (a power of two: exact)
                     const float y = qx[i].get(key_channel<KB>(j)) * down;
                     const _Float16 hi = (_Float16)y;
                     q_hi[i][j] = hi;
@@ -686,7 +696,7 @@ void attend_kernel(const Attend a) {
                         z = __builtin_fmaf(step, kCentreV, z);
                     sum_p += p;
                     sum_z = __builtin_fmaf(p, z, sum_z);
-                    const float w = p * step;
+                    const float w = kTwoW ? rounded(p * step) : p * step;
                     const _Float16 hi = (_Float16)w;
                     w_hi[4 * s + i] = hi;
                     if constexpr (kTwoW)

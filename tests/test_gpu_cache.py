@@ -294,6 +294,21 @@ def test_attend_split_sequences(kind, batch, longest):
             kind=kind)
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+@pytest.mark.parametrize("vbits", [8, 4])
+def test_attend_weights_next_to_ties(kind, vbits):
+    """96 Ki weights, some of which lie next to a tie of their first term's
+    rounding: the two terms together are the weight all the same.  Logits are
+    small, so that they add next to nothing to the bound."""
+    say(kind, vbits)
+    rng = np.random.default_rng(vbits)
+    f = Filled(rng, 30, 2, 16, 64, 8, vbits)
+    table = rng.integers(0, 30, (64, 3)).astype(np.int32)
+    f.check(queries(rng, 64, 64, 64, kind), torch.from_numpy(table).cuda(),
+            torch.full((64,), 24, dtype=torch.int32, device="cuda"),
+            scale=2e-3, kind=kind)
+
+
 @pytest.mark.parametrize("batch", [64, 65, 300, 4096, 4500])
 def test_attend_many_sequences(batch):
     """More sequences than lanes of a wave, more than 64 for a lane; most of
