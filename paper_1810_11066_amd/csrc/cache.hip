@@ -55,6 +55,27 @@ __device__ __forceinline__ float larger(float a, float b) {
     return __builtin_amdgcn_fmed3f(a, b, kBig);
 }
 
+// 1 / s, rounded to nearest, of a bfloat16 s of 2^-60 to 2^124.  v_rcp_f32 is within
+// an ulp, so e = 1 - s r is below 2^-22 and exact (8 bits times 24), and r + e r
+// is 1 / s but for e^2, 2^-21 of an ulp, and its own rounding; 1 / s itself is
+// a power of two or, s having 8 bits, 1/510 of an ulp or more from a tie.  (The
+// division takes 10 instructions, this 3.)
+__device__ __forceinline__ float reciprocal(float s) {
+    const float r = __builtin_amdgcn_rcpf(s);
+    return __builtin_fmaf(__builtin_fmaf(-s, r, 1.0f), r, r);
+}
+
+// Smallest and largest of 8 values.
+__device__ __forceinline__ void extremes(const float (&x)[8], float& lo,
+                                         float& hi) {
+    lo = hi = x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        lo = fminf(lo, x[i]);
+        hi = fmaxf(hi, x[i]);
+    }
+}
+
 // Which rows a wave has: all tokens of a stretch for one (head, side).
 struct RowsGrid {
     int64_t tokens;
@@ -110,13 +131,15 @@ __device__ __forceinline__ void stream(V* p, V v) {
     __builtin_nontemporal_store(v, p);
 }
 
-// Bound by memory, and next by the vector ALUs (about 130 instructions for 8
+// Bound by memory, and next by the vector ALUs (about 120 instructions for 8
 // channels a lane: 16 bytes of float16): 100000 tokens of 8 heads of 128, 570
 // MB, in 114.6 us = 5.0 TB/s.  Codes are stored the ordinary way: past the
 // caches a write by itself takes 0 to 5 us less (60000 tokens of 8 heads of 64
 // 37.2 for 41.4 us), but the read or the attention that comes next finds them in
 // the caches (write and read of those together 66.6 us, 75.8 past the caches; of
-// 16384 tokens of 4-bit codes, 128 channels 34.6 and 39.8).
+// 16384 tokens of 4-bit codes, 128 channels 34.6 and 39.8).  NaN and infinities
+// are looked for in a sum, and the values mended in the waves that have any; that
+// and the short reciprocal took those 16384 tokens from 20.4 to 17.8 us.
 template <int T, int LPR, int STEPS>
 __global__ __launch_bounds__(kBlock) void write_kernel(
     Pages c, const void* __restrict__ k, const void* __restrict__ v,
@@ -146,14 +169,21 @@ __global__ __launch_bounds__(kBlock) void write_kernel(
     }
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        float x[8];
+        float x[8], lo, hi, sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = finite(in[s].get(i));
-        float lo = x[0], hi = x[0];
+        for (int i = 0; i < 8; ++i) {
+            x[i] = in[s].get(i);
+            sum += x[i];
+        }
+        extremes(x, lo, hi);
+        // a NaN or an infinity among the values shows in their sum (finite
+        // values' may show too: they come out as they were)
+        const bool odd = !(fabsf(sum) <= kBig) ||
+                         (T != kF16 && !(fmaxf(hi, -lo) <= kBig));
+        if (__any(odd)) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) {
-            lo = fminf(lo, x[i]);
-            hi = fmaxf(hi, x[i]);
+            for (int i = 0; i < 8; ++i) x[i] = finite(x[i]);
+            extremes(x, lo, hi);
         }
         if (!mine) lo = kBig, hi = -kBig;
         lo = reduce_row<LPR>(lo, smaller);
@@ -164,9 +194,10 @@ __global__ __launch_bounds__(kBlock) void write_kernel(
         const uint32_t zb = lcut + (lcut != lb && (lb >> 31) ? 0x10000u : 0u);
         const float z = bits_f32(zb);
         const uint32_t rb = f32_bits((hi - z) * per), rcut = rb & 0xFFFF0000u;
-        const float s0 = bits_f32(rcut + (rcut != rb ? 0x10000u : 0u));
-        const float step = fmaxf(s0, 0x1p-60f);
-        const float inv = 1.0f / step;
+        // (not negative: bits compare as the values do)
+        const uint32_t sb = max(rcut + (rcut != rb ? 0x10000u : 0u),
+                                f32_bits(0x1p-60f));
+        const float inv = reciprocal(bits_f32(sb));
         if (slot[s] < c.slots && mine) {
             const uint32_t page = c.by_page.div(slot[s]);
             const int64_t row =
@@ -179,7 +210,7 @@ __global__ __launch_bounds__(kBlock) void write_kernel(
                 *reinterpret_cast<uint32_t*>(codes + row * (c.dim >> 1) +
                                              (channel >> 1)) =
                     nibbles(d[0]) | nibbles(d[1]) << 16;
-            if (part == 0) c.steps[side][row] = f32_bits(step) >> 16 | zb;
+            if (part == 0) c.steps[side][row] = sb >> 16 | zb;
         }
     }
 }

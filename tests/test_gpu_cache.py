@@ -178,6 +178,62 @@ def test_read_values(tokens, kind):
         assert torch.equal(got.cpu(), want)
 
 
+def same_bytes(cache, x, bits):
+    """The cache, its slots 0.. written with rows x, holds the definition's
+    codes, steps and offsets (-0 and 0 are the same offset)."""
+    with np.errstate(all="ignore"):
+        c, s, z = ref.quantize(x, bits)
+    n = len(x)
+    for codes, steps in (cache[:2], cache[2:]):
+        got = codes.transpose(1, 2).flatten(0, 1)[:n].cpu().numpy()
+        assert np.array_equal(got, ref.join_codes(c, bits))
+        got = steps.float().transpose(1, 2).flatten(0, 1)[:n].cpu().numpy()
+        assert np.array_equal(got[..., 0], s)
+        assert np.array_equal(got[..., 1], z)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_write_every_step(bits):
+    """Steps of every bfloat16 mantissa and of exponents from the smallest to
+    the largest, with values next to the middle between two codes."""
+    top = 2 ** bits - 1
+    e = np.concatenate([np.arange(-60, -50), np.arange(-50, 110, 7),
+                        np.arange(110, 118)])
+    s = ((1 + np.arange(128) / 128) * 2.0 ** e[:, None]).ravel()
+    part = (np.arange(14) + 0.5) * top / 14
+    near = np.concatenate([[0.0, top - 0.25], np.floor(part) + 0.5 +
+                           2.0 ** -18 * (np.arange(14) % 3 - 1)])
+    x = (s[:, None] * near).astype(np.float32)[:, None]
+    pages = len(x) // 64 + 1
+    cache = kc.empty(pages, 1, 64, 16, bits, bits)
+    k = torch.from_numpy(x).cuda()
+    kc.write(k, k, torch.arange(len(x), dtype=torch.int32, device="cuda"),
+             cache)
+    same_bytes(cache, x, bits)
+    assert len(np.unique(ref.quantize(x, bits)[1])) > 128 * (len(e) - 2)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_write_odd_values_among_others(kind):
+    """NaN, infinities and the largest values, alone in a row of a wave, several
+    that cancel in a sum, and rows whose sum overflows though none does."""
+    rng = np.random.default_rng(3)
+    big = 65504.0 if kind == "f16" else 3.0e38
+    x = rng.standard_normal((60, 1, 48))
+    x[3, 0, 40] = np.nan
+    x[9, 0, 0], x[9, 0, 1] = np.inf, -np.inf
+    x[14, 0, 7], x[14, 0, 6] = big, -big
+    x[20] = big / 4
+    x[25, 0, :24], x[25, 0, 24:] = big / 2, -big / 2
+    x[33, 0, 47] = -np.inf
+    x[41] = np.nan
+    x[47] = np.inf
+    xh, xd = rounded(x, kind)
+    cache = kc.empty(4, 1, 16, 48, 8, 8)
+    kc.write(xd, xd, torch.arange(60, dtype=torch.int32, device="cuda"), cache)
+    same_bytes(cache, xh, 8)
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 def test_values_within_half_a_step(bits):
     """A value is off by at most s / 2 and a few units of binary32 of the
