@@ -125,7 +125,7 @@ __device__ __forceinline__ uint32_t spread(uint32_t w) {
 
 // Values read back go past the caches (non-temporal stores): they push out
 // nothing that is read sooner (16384 tokens of 8 heads of 128 in 17.1
-// us, 24.4 without; 100000 in 108.7 and 117.6).
+// us, 24.3 without; 100000 in 108 and 118).
 template <class V>
 __device__ __forceinline__ void stream(V* p, V v) {
     __builtin_nontemporal_store(v, p);
@@ -133,13 +133,13 @@ __device__ __forceinline__ void stream(V* p, V v) {
 
 // Bound by memory, and next by the vector ALUs (about 120 instructions for 8
 // channels a lane: 16 bytes of float16): 100000 tokens of 8 heads of 128, 570
-// MB, in 114.6 us = 5.0 TB/s.  Codes are stored the ordinary way: past the
+// MB, in 116 us = 4.9 TB/s.  Codes are stored the ordinary way: past the
 // caches a write by itself takes 0 to 5 us less (60000 tokens of 8 heads of 64
-// 37.2 for 41.4 us), but the read or the attention that comes next finds them in
-// the caches (write and read of those together 66.6 us, 75.8 past the caches; of
-// 16384 tokens of 4-bit codes, 128 channels 34.6 and 39.8).  NaN and infinities
+// 36.9 for 41.3 us), but the read or the attention that comes next finds them in
+// the caches (write and read of those together 66.6 us, 75.5 past the caches; of
+// 16384 tokens of 4-bit codes, 128 channels 32.4 and 37.4).  NaN and infinities
 // are looked for in a sum, and the values mended in the waves that have any; that
-// and the short reciprocal took those 16384 tokens from 20.4 to 17.8 us.
+// and the short reciprocal took those 16384 tokens from 20.4 to 17.9 us.
 template <int T, int LPR, int STEPS>
 __global__ __launch_bounds__(kBlock) void write_kernel(
     Pages c, const void* __restrict__ k, const void* __restrict__ v,
@@ -389,8 +389,8 @@ hipError_t launch_write(const Pages& c, const void* k, const void* v,
                         const int32_t* slots, int64_t tokens,
                         hipStream_t st) {
     int lpr, steps;
-    // (8192 tokens, 32 waves a SIMD: 11.9 us single, 12.5 in twos; 16384: 22.0
-    // and 20.5; in fours 13.1 and 21.0)
+    // (8 heads of 128 to 8 bits, 8192 tokens, 32 waves a SIMD: 11.4 us single,
+    // 12.1 in twos; 16384: 24.3 and 23.2; to 4 bits 19.6 and 17.8)
     const RowsGrid g = rows_grid(c, tokens, 32, &lpr, &steps);
     return pick<Write>(dtype, lpr, steps, c, k, v, k_stride, v_stride, slots,
                        g, st);
@@ -399,8 +399,8 @@ hipError_t launch_write(const Pages& c, const void* k, const void* v,
 hipError_t launch_read(const Pages& c, const int32_t* slots, int64_t tokens,
                        void* k, void* v, int dtype, hipStream_t st) {
     int lpr, steps;
-    // (1024 tokens of 8 heads of 128, 4 waves a SIMD: 3.3 us single, 3.4 in
-    // twos; 2048: 4.2 and 3.9; 100000: 137 and 108; in fours 3.8, 4.1 and 107)
+    // (1024 tokens of 8 heads of 128, 4 waves a SIMD: 3.4 us single, 3.5 in
+    // twos; 2048: 4.1 and 3.9; 8192: 10.3 and 9.9; 100000: 139 and 108)
     const RowsGrid g = rows_grid(c, tokens, 7, &lpr, &steps);
     return pick<Read>(dtype, lpr, steps, c, slots, k, v, g, st);
 }
