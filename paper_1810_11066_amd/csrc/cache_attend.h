@@ -19,10 +19,12 @@
 //
 // Codes become float16 without conversions.  For 16-bit calls a code's own bits
 // are the operand: as a float16 they are the subnormal c 2^-24, which the
-// matrix unit multiplies exactly (one byte permutation for two codes).  4-bit
-// codes are taken as 16 c: the unit aligns products by the operands' exponents,
-// and the leading zeros of a subnormal are bits that it loses of the sum (with
-// c as it is lse was off by 2 to 4 10^-6, now by up to 4 10^-7).  float32 calls
+// matrix unit multiplies exactly (one byte permutation for two codes).  The unit
+// aligns products by the operands' exponents, and the leading zeros of a
+// subnormal are bits that it loses of the sum; so 4-bit codes are taken as 16 c
+// and 8-bit keys as 4 c, a shift more for two of them (4-bit keys as c: lse off
+// by 2 to 4 10^-6, 8-bit ones as c: up to 9 10^-7, now 5 10^-7 and less; 8-bit
+// calls of one unit take 1 % longer for it, long ones as long).  float32 calls
 // centre the codes: 0x6400 | c is 1024 + c, and one packed subtraction of 1024 +
 // centre (128; 8 of the 4-bit ones) gives c' = c - centre exactly, so that sums
 // do not grow by the offset and cancel again.  With z' = z + centre s (centre 0
@@ -204,17 +206,18 @@ __device__ __forceinline__ uint32_t high_nibbles(uint32_t x) {
 }
 
 // Channel-major operand of the keys: 8 codes of one token.  8 bits: 4 in x, 4
-// in y, in order; 4 bits: all in x, in the order 0 2 4 6 1 3 5 7.
+// in y, in order (as 4 c where they are not centred); 4 bits: all in x, in the order 0 2 4 6 1 3 5 7.
 template <int BITS, bool CENTRED>
 __device__ __forceinline__ half8v key_operand(uint32_t x, uint32_t y) {
     if constexpr (BITS == 4) {
         y = high_nibbles(x);
         x = low_nibbles(x);
     }
-    const u32x4 f = {byte_pair<0, 1, CENTRED>(x, x),
-                     byte_pair<2, 3, CENTRED>(x, x),
-                     byte_pair<0, 1, CENTRED>(y, y),
-                     byte_pair<2, 3, CENTRED>(y, y)};
+    u32x4 f = {byte_pair<0, 1, CENTRED>(x, x),
+               byte_pair<2, 3, CENTRED>(x, x),
+               byte_pair<0, 1, CENTRED>(y, y),
+               byte_pair<2, 3, CENTRED>(y, y)};
+    if constexpr (BITS == 8 && !CENTRED) f <<= 2;
     return __builtin_bit_cast(half8v, f);
 }
 // Channel of element e (0..7) of that operand.
@@ -368,7 +371,7 @@ void attend_kernel(const Attend a) {
     constexpr float kCentreV = !kCentred ? 0.0f : VB == 8 ? 128.0f : 8.0f;
     // codes over what they are as float16
     constexpr float kCode = kCentred ? 1.0f : 0x1p24f;
-    constexpr float kCodeK = KB == 8 ? kCode : kCode / 16;
+    constexpr float kCodeK = KB == 4 ? kCode / 16 : kCentred ? kCode : kCode / 4;
     constexpr float kCodeV = VB == 8 ? kCode : kCode / 16;
     __shared__ float sm_o[kWaves][16][DP + 4];
     __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
