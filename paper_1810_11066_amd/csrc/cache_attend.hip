@@ -104,21 +104,24 @@ template <> hipError_t launch_attend_dp<256>(const Attend&, hipStream_t);
 // How a call is shared out, by what the host knows: the pairs of sequences and
 // head tiles, and the tokens that the longest sequence may span.
 //
-// A pair to one workgroup needs no plan of the lengths and no join (4.4 us and a
-// launch), but the longest pair sets the time: 4.5 us and 1 us a unit of 128
-// tokens.  Up to 4 units that is always shorter (8 pairs of 4 units 8.9 us whole
-// and 9.7 shared, of 8 units 13.1 and 10.6).  Longer ones win where the pairs
-// fill the GPU anyway: up to 8 units with a pair for every CU (320 pairs of 8
-// units 22 and 25 us), up to 16 with pairs for half of the workgroups that run
-// at once (512 pairs of 16 units, 64 channels 32 and 40 us); a batch with one
-// long sequence among short ones loses at most the time of those units.
+// A pair to one workgroup needs no plan of the lengths and no join (4 us and a
+// launch), but the longest pair sets the time: 4 us and 1.3 us a unit of
+// 128 tokens.  Up to 4 units that is always shorter (8 pairs of 4 units 8.8 us whole
+// and 9.8 shared, of 8 units 14.5 and 9.9; 128 pairs of 4 units 10.1 and 12.6).
+// Longer ones win where the pairs fill the GPU anyway: up to 8 units with a pair
+// for every CU (320 pairs of 8 units 22.0 and 24.9 us), up to 16 with pairs for
+// half of the workgroups that run at once (512 pairs of 16 units 56 and 60 us, 64
+// channels 31.7 and 33.3).  Lengths from a quarter of the longest to all of it
+// leave that so (384 pairs of 375 to 1500 tokens 27.5 and 27.2, 2000 pairs 112 and
+// 119); where few are long, what the longest takes is lost (lengths spread by
+// their logarithm from 1: to 1000 tokens 16.5 and 16.8, to 2000 27.8 and 18.5).
 //
 // With fewer pairs than CUs a workgroup can have its CU to itself: the wide
 // form, of as many waves as the CU holds (8 to 16).  A CU's own rate of reading
 // bounds it, so it needs pairs on a quarter of the CUs, and sequences of more
-// than 4 units that it takes in 4 steps (128 pairs of 700 tokens 11.3 us wide,
-// 15.1 shared; of 1024 13.4 and 17.8; of 2048 no difference; 8 pairs of 800
-// tokens 12.2 and 10.6).
+// than 4 units that it takes in 4 steps (128 pairs of 748 tokens 11.7 us wide,
+// 14.4 shared; of 1132 13.9 and 16.9; of 1516 16.6 and 18.2; 64 pairs 11.1 and
+// 12.0, 13.5 and 14.0, 16.1 and 14.6).
 //
 // Everything else is shared: as many workgroups as run at once, each with its
 // part (4 times as many, taken up as others end: 551 us for 524 at 128
