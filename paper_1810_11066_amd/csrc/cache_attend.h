@@ -36,9 +36,9 @@
 // float16: bfloat16 and float16 values keep all their bits, but for what lies
 // below 2^-30 of the row's largest; float32 queries take a second float16 for
 // the rest (22 bits together), a second MFMA into the same accumulator.  w is
-// rounded to float16 for bfloat16 calls: 2^-12 of w c, 3 times the spread of
-// the values where codes are not centred, against the output's own 2^-9.
-// float16 and float32 calls take a second float16 for the rest of w.
+// two float16 as well, 22 bits.  (One was 2^-12 of w c, whose magnitudes are 3
+// times the spread of the values where codes are not centred: bfloat16 outputs
+// came out a step off.)
 // w = 2^7 (p / 2^m) (s / S) with m the running maximum and S a power of two
 // above every s, and 2^-10 |z|, so far (z far beyond s is a row of nearly equal
 // values, whose sums p z would leave binary32); m may lag by 2^8, so w stays
@@ -366,7 +366,7 @@ void attend_kernel(const Attend a) {
     const bool one = WIDE || a.whole;           // every pair one workgroup's
     constexpr int kSteps = DP / 32;             // MFMAs of the logits
     constexpr int kOwn = C::kOwn;
-    constexpr bool kTwoQ = T == kF32, kTwoW = T != kBF16, kCentred = T == kF32;
+    constexpr bool kTwoQ = T == kF32, kCentred = T == kF32;
     constexpr float kCentreK = !kCentred ? 0.0f : KB == 8 ? 128.0f : 8.0f;
     constexpr float kCentreV = !kCentred ? 0.0f : VB == 8 ? 128.0f : 8.0f;
     // codes over what they are as float16
@@ -699,11 +699,10 @@ void attend_kernel(const Attend a) {
                         z = __builtin_fmaf(step, kCentreV, z);
                     sum_p += p;
                     sum_z = __builtin_fmaf(p, z, sum_z);
-                    const float w = kTwoW ? rounded(p * step) : p * step;
+                    const float w = rounded(p * step);
                     const _Float16 hi = (_Float16)w;
                     w_hi[4 * s + i] = hi;
-                    if constexpr (kTwoW)
-                        w_lo[4 * s + i] = (_Float16)(w - (float)hi);
+                    w_lo[4 * s + i] = (_Float16)(w - (float)hi);
                 }
             if (more) load_steps(next);
 
@@ -715,7 +714,7 @@ void attend_kernel(const Attend a) {
                 for (int e = 0; e < 4; ++e) {
                     f32x4& sum = o[first + e * by];
                     sum = mfma(f[e], w_hi, sum);
-                    if constexpr (kTwoW) sum = mfma(f[e], w_lo, sum);
+                    sum = mfma(f[e], w_lo, sum);
                 }
             };
             if constexpr (VB == 8) {
