@@ -39,11 +39,16 @@
 // two float16 as well, 22 bits.  (One was 2^-12 of w c, whose magnitudes are 3
 // times the spread of the values where codes are not centred: bfloat16 outputs
 // came out a step off.)
-// w = 2^7 (p / 2^m) (s / S) with m the running maximum and S a power of two
-// above every s, and 2^-10 |z|, so far (z far beyond s is a row of nearly equal
-// values, whose sums p z would leave binary32); m may lag by 2^8, so w stays
-// below 2^15 and keeps its full precision down to 2^-21 of the largest weight.
-// Everything else is float32.
+// Weights and the softmax's sum have references of their own.  p = 2^(logit - m),
+// m 24 below the running maximum in whole numbers, so that what float32 drops is
+// 2^-150 of the largest and less.  w = 2^k p s, with k such that the largest
+// p max(s, 2^-10 |z|) so far makes 2^6 to 2^7: a row counts by what is attended
+// to of it, and one that is not, however wide, takes no bits from the others.
+// (2^-10 |z|: z far beyond s is a row of nearly equal values, whose sums 2^k p z
+// would leave float32.  It is looked at only where a sum gets large.)  Both lag
+// by up to 2^8, so w stays below 2^15 and keeps its 22 bits down to 2^-17 of
+// the largest, and is rounded to 2^-31 of it below.  A partial result is the mean
+// of its own tokens, with m and the sum of p.  Everything else is float32.
 //
 // Sharing: the units of all (sequence, head tile) pairs are numbered in one row
 // of places, and workgroup i of n takes the places [i U / n, (i + 1) U / n):
@@ -65,7 +70,13 @@
 
 namespace bscache {
 
-constexpr float kNone = -3.0e38f;       // maximum of no logits
+constexpr float kNone = -3.0e38f;       // reference of no logits
+// The reference m is so far below the running maximum.
+constexpr float kBelow = 24.0f;
+// k of the first tokens: the largest p is above 2^(kBelow - 1), a step at least
+// 2^-60.
+constexpr int kMost = 44;
+constexpr int kSmall = -64;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // ---- the row of units ------------------------------------------------------
@@ -167,7 +178,8 @@ __device__ __forceinline__ int32_t range_start(int32_t i, int32_t u, int32_t n) 
 }
 // Partial results: slot 2 i of workgroup i for the pair that began before its
 // range, 2 i + 1 for the pair that goes on behind it.  A slot holds [16][dim]
-// sums and [16][2] maximum (of mo, see below) and sum of weights.
+// means and [16][2] reference and sum of p, 2^kSmall of it (the join's sums of
+// products with values near the largest stay within float32).
 // Behind the slots, for every pair: the workgroups of its first and last units.
 __host__ __device__ __forceinline__ int64_t part_bytes(int32_t dim) {
     return 64 * (dim + 2);
@@ -269,16 +281,21 @@ __device__ __forceinline__ void store_out(void* out, int64_t at, int dtype,
     }
 }
 
-// Writes 4 channels of a row of the output, and its lse.
+// Quotient of 4 sums and the sum of weights: 0 where there are none.
+__device__ __forceinline__ f32x4 mean(f32x4 r, float l) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = l == 0.0f ? 0.0f : r[e] / l;
+    return r;
+}
+
+// Writes 4 channels of a row of the output, and its lse: of p with reference m
+// and sum l.
 __device__ __forceinline__ void finish(const Attend& a, int dtype, int64_t row,
                                        int d, float m, float l, f32x4 r) {
-    const bool none = l == 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = none ? 0.0f : r[e] / l;
     store_out(a.out, row * a.c.dim + d, dtype, r);
     if (d == 0 && a.lse)
-        a.lse[row] = none ? -INFINITY
-                          : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        a.lse[row] = l == 0.0f ? -INFINITY
+                               : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // ---- the kernel ------------------------------------------------------------
@@ -375,6 +392,7 @@ void attend_kernel(const Attend a) {
     constexpr float kCodeV = VB == 8 ? kCode : kCode / 16;
     __shared__ float sm_o[kWaves][16][DP + 4];
     __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
+    __shared__ int sm_k[kWaves][16];
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -601,11 +619,10 @@ void attend_kernel(const Attend a) {
         f32x4 o[kOwn];
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) o[j] = f32x4{0, 0, 0, 0};
-        float top = kNone;          // running maximum m of the logits
-        float s_top = 0.0f;         // S: a power of two, above every s and
-                                    // 2^-10 |z| so far
-        float mo = kNone;           // m + log2 S - 7
-        float sum_p = 0.0f, sum_z = 0.0f;
+        float m = kNone;            // reference of p, a whole number
+        int k = kMost;              // of the weights: w = 2^k p s
+        float sum_p = 0.0f;
+        float sum_z = 0.0f;         // of 2^k p z
 
         for (int32_t c = c0; c < c1; ++c) {
             // ---- logits
@@ -656,54 +673,83 @@ void attend_kernel(const Attend a) {
                         z = __builtin_fmaf(step, kCentreK, z);
                     x[s][i] = __builtin_fmaf(step, acc[s][i], z * q_sum);
                 }
-            float big = -INFINITY, s_big = 0.0f, z_big = 0.0f;
+            float big = -INFINITY;
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    big = fmaxf(big, x[s][i]);
-                    s_big = fmaxf(s_big, step_of(vs[s][i]));
-                    z_big = fmaxf(z_big, fabsf(offset_of(vs[s][i])));
-                }
+                for (int i = 0; i < 4; ++i) big = fmaxf(big, x[s][i]);
             big *= q_scale;
-            s_big = fmaxf(s_big, z_big * 0x1p-10f);
-            if (__any(big > top + 8.0f || s_big > s_top)) {
-                top = fmaxf(top, over_groups(big, larger));
-                float s_all = over_groups(s_big, larger);
-#pragma unroll
-                for (int d = 1; d < 16; d *= 2)
-                    s_all = fmaxf(s_all, __shfl_xor(s_all, d));
-                // (at least 2^-60: the quantizer's smallest step)
-                const uint32_t e = max(f32_bits(s_all) >> 23, 127u - 61u) + 1;
-                s_top = fmaxf(s_top, bits_f32(e << 23));
-                const float lift =
-                    (float)((int)(f32_bits(s_top) >> 23) - 127 - 7);
-                const float mo_new = top + lift;
-                const float f = __builtin_amdgcn_exp2f(mo - mo_new);
-                mo = mo_new;
-                sum_p *= f;
+            if (__any(big > m + (kBelow + 8.0f))) {
+                const float m_new =
+                    fmaxf(m, ceilf(over_groups(big, larger)) - kBelow);
+                // (from kNone: more than any exponent)
+                const int up = (int)fminf(m_new - m, 2000.0f);
+                // what p falls by the weights keep, as far as k goes
+                const int k_new = min(k + up, kMost);
+                const float f = ldexpf(1.0f, k_new - k - up);
+                sum_p *= ldexpf(1.0f, -up);
                 sum_z *= f;
 #pragma unroll
                 for (int j = 0; j < kOwn; ++j) o[j] *= f;
+                m = m_new;
+                k = k_new;
             }
+            float p[8], w[8], z_next;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(
+                    __builtin_fmaf(x[i >> 2][i & 3], q_scale, -m));
+                sum_p += p[i];
+            }
+            auto offset = [&](int i) {
+                const float z = offset_of(vs[i >> 2][i & 3]);
+                return kCentred ? __builtin_fmaf(step_of(vs[i >> 2][i & 3]),
+                                                 kCentreV, z)
+                                : z;
+            };
+            auto weigh = [&] {
+                z_next = sum_z;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float t = ldexpf(p[i], k);
+                    w[i] = rounded(t * step_of(vs[i >> 2][i & 3]));
+                    z_next = __builtin_fmaf(t, offset(i), z_next);
+                }
+            };
+            weigh();
+            float w_big = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w_big = fmaxf(w_big, w[i]);
+            if (__any(w_big > 0x1p15f || !(fabsf(z_next) <= 0x1p100f))) {
+                float most = 0.0f;          // of 2^-64 p max(s, 2^-10 |z|)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    most = fmaxf(most,
+                                 ldexpf(p[i], -64) *
+                                     fmaxf(step_of(vs[i >> 2][i & 3]),
+                                           fabsf(offset(i)) * 0x1p-10f));
+                // these, and the sum, are below 2^e
+                const int e = (int)(f32_bits(over_groups(most, larger)) >> 23) -
+                              126 + 64;
+                const int e_z =
+                    (int)(f32_bits(over_groups(fabsf(sum_z), larger)) >> 23) -
+                    126;
+                const int k_new = min(k, min(7 - e, k + 40 - e_z));
+                const float f = ldexpf(1.0f, k_new - k);
+                sum_z *= f;
+#pragma unroll
+                for (int j = 0; j < kOwn; ++j) o[j] *= f;
+                k = k_new;
+                weigh();
+            }
+            sum_z = z_next;
             half8v w_hi, w_lo;
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(
-                        __builtin_fmaf(x[s][i], q_scale, -mo));
-                    const float step = step_of(vs[s][i]);
-                    float z = offset_of(vs[s][i]);
-                    if constexpr (kCentred)
-                        z = __builtin_fmaf(step, kCentreV, z);
-                    sum_p += p;
-                    sum_z = __builtin_fmaf(p, z, sum_z);
-                    const float w = rounded(p * step);
-                    const _Float16 hi = (_Float16)w;
-                    w_hi[4 * s + i] = hi;
-                    w_lo[4 * s + i] = (_Float16)(w - (float)hi);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const _Float16 hi = (_Float16)w[i];
+                w_hi[i] = hi;
+                w_lo[i] = (_Float16)(w[i] - (float)hi);
+            }
             if (more) load_steps(next);
 
             // ---- values
@@ -760,8 +806,9 @@ void attend_kernel(const Attend a) {
         const int end_lane = here(lane);
         const int col = end_lane & 15, quarter = end_lane >> 4;
         if (quarter == 0) {
-            sm_m[wave][col] = mo;
+            sm_m[wave][col] = m;
             sm_l[wave][col] = sum_p;
+            sm_k[wave][col] = k;
         }
         // o[j][i] is channel kOwn (4 (lane / 16) + i) + j of head lane % 16
 #pragma unroll
@@ -784,27 +831,38 @@ void attend_kernel(const Attend a) {
         const int quads = dim >> 2;
         for (int n = 64 * wave + end_lane; n < heads * quads; n += kThreads) {
             const int h = n / quads, d = 4 * (n - h * quads);
-            float m = sm_m[0][h];
+            float top = sm_m[0][h];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm_m[w][h]);
+            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sm_m[w][h]);
+            // a wave's sums are its means times 2^(k + its p's): the largest
+            // of the factors that bring them to p of `top`, then the sums
+            int down = -4000;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w)
+                down = max(down, (int)fmaxf(sm_m[w][h] - top, -2000.0f) -
+                                     sm_k[w][h]);
             f32x4 r = {0, 0, 0, 0};
             float l = 0.0f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const float f = __builtin_amdgcn_exp2f(sm_m[w][h] - m);
-                l = __builtin_fmaf(f, sm_l[w][h], l);
+                const int by = (int)fmaxf(sm_m[w][h] - top, -2000.0f);
+                const float f = ldexpf(1.0f, by - sm_k[w][h] - down);
+                l = __builtin_fmaf(ldexpf(1.0f, by), sm_l[w][h], l);
                 const f32x4 y =
                     *reinterpret_cast<const f32x4*>(&sm_o[w][h][d]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) r[e] = __builtin_fmaf(f, y[e], r[e]);
             }
+            r = mean(r, l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = ldexpf(r[e], down);
             if (is_whole) {
-                finish(a, T, row0 + h, d, m, l, r);
+                finish(a, T, row0 + h, d, top, l, r);
             } else {
                 *reinterpret_cast<f32x4*>(part + h * dim + d) = r;
                 if (d == 0)
                     *reinterpret_cast<float2*>(part + 16 * dim + 2 * h) =
-                        make_float2(m, l);
+                        make_float2(top - (float)kSmall, ldexpf(l, kSmall));
             }
         }
         if (last) break;

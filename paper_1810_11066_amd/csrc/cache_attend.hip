@@ -67,8 +67,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a) {
             r *= f;
 #pragma unroll
             for (int u = 0; u < kDeep; ++u) {
-                const float g = __builtin_amdgcn_exp2f(ml[u].x - top);
-                l = __builtin_fmaf(g, ml[u].y, l);
+                const float g = __builtin_amdgcn_exp2f(ml[u].x - top) * ml[u].y;
+                l += g;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     r[e] = __builtin_fmaf(g, y[u][e], r[e]);
@@ -91,7 +91,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a) {
                 }
             }
         }
-        if (on && mine == 0) finish(a, a.dtype, row0 + h, d, m, l, r);
+        if (on && mine == 0)
+            finish(a, a.dtype, row0 + h, d, m, l, mean(r, l));
     }
 }
 

@@ -46,3 +46,96 @@ def test_bfloat16_outputs_are_the_result_rounded_once(dim, vbits):
             half = 2.0 ** (np.floor(np.log2(np.abs(o) + more)) - 8)
             off = np.abs(got[b, h] - o)
             assert (off <= half + more).all(), (b, h, (off - half).max())
+
+
+# ---- rows of one sequence far apart in size ----------------------------------
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("vbits", [8, 4])
+@pytest.mark.parametrize("size", [2.0 ** 15, 2.0 ** 22, 2.0 ** 30, np.inf])
+def test_a_wide_row_that_nobody_attends_to(kind, vbits, size):
+    """One token of 40 with a logit 100 lower and values `size` times larger
+    (an infinity is kept as 2^126) leaves the others' weights as they are, at
+    each place in a wave's tile, among the first tokens and the last."""
+    say(kind, vbits, size)
+    rng = np.random.default_rng(7)
+    n, dim = 48, 64
+    q = rounded(np.ones((6, 1, dim)) * 0.5, kind)[1]
+    k = rng.standard_normal((6 * n, 1, dim)) * 0.05
+    v = rng.standard_normal((6 * n, 1, dim))
+    for b, at in enumerate((0, 5, 17, 31, 33, 39)):
+        k[b * n + at] = -25.0                   # 0.5 * 64 * 25 / 8 = 100
+        if np.isinf(size):
+            v[b * n + at, 0, 3] = np.inf
+        else:
+            v[b * n + at] *= size
+    with np.errstate(all="ignore"):
+        f = Filled(rng, 18, 1, 16, dim, 8, vbits, rows=[k, v])
+    f.check(q, on(np.arange(18).reshape(6, 3)), on([40] * 6), kind=kind)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_wide_rows_in_other_waves_and_workgroups(kind):
+    """The same in a sequence that several workgroups share: waves and partial
+    results of different references are joined."""
+    say(kind)
+    rng = np.random.default_rng(8)
+    n, dim = 3000, 64
+    q = rounded(np.ones((1, 2, dim)) * 0.5, kind)[1]
+    k = rng.standard_normal((n + 8, 1, dim)) * 0.05
+    v = rng.standard_normal((n + 8, 1, dim))
+    for at, size in ((10, 2.0 ** 26), (700, 2.0 ** 40), (1500, 2.0 ** 100),
+                     (2999, 2.0 ** 30)):
+        k[at] = -30.0
+        v[at] *= size
+    f = Filled(rng, 188, 1, 16, dim, 8, 8, rows=[k, v])
+    assert " shared " in kc.describe(188, 1, 16, dim, 1, 2, 188 * 16,
+                                     dtype=DTYPE[kind])
+    f.check(q, on(np.arange(188)[None]), on([n]), kind=kind)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [7, 300, 3000])
+def test_values_at_the_ends(kind, n):
+    """Rows of the largest values attended to beside ordinary ones, nothing but
+    the largest, constant rows (steps of 2^-60) of large, alternating and tiny
+    values: outputs are the mean, and lse knows nothing of the values."""
+    say(kind, n)
+    rng = np.random.default_rng(n)
+    dim, pages = 64, -(-n // 16)
+    k = rng.standard_normal((16 * pages, 1, dim))
+    q = queries(rng, 1, 3, dim, kind)
+    table, lengths = on(np.arange(pages)[None]), on([n])
+    lse = []
+    some = rng.standard_normal((16 * pages, 1, dim))
+    one = some.copy()
+    one[n // 2] = np.inf
+    sign = np.where(np.arange(16 * pages) % 2, 1.0, -1.0)[:, None, None]
+    for v in (some, one, np.full_like(some, np.inf), np.full_like(some, 1e30),
+              sign * np.full_like(some, 1e30), np.full_like(some, 1e-30),
+              some * 1e34, some * 1e-15,
+              np.where(np.arange(16 * pages)[:, None, None] < n // 2, 1e36,
+                       some)):
+        with np.errstate(all="ignore"):
+            f = Filled(rng, pages, 1, 16, dim, 8, 8, rows=[k, v])
+        lse.append(f.check(q, table, lengths, kind=kind)[1])
+    for other in lse[1:]:
+        assert np.array_equal(lse[0], other)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_logits_that_rise_and_wide_rows_that_fade(kind):
+    """Logits rise by up to 300 along the sequence while the steps fall and
+    rise: a reference that was set by a token long past does not last."""
+    say(kind)
+    rng = np.random.default_rng(9)
+    n, dim = 480, 64
+    rise = np.linspace(0, 1, n)
+    q = rounded(np.ones((1, 4, dim)) * np.array([0.0, 0.1, 0.5, -0.5])
+                [None, :, None], kind)[1]
+    k = rng.standard_normal((n, 1, dim)) * 0.01 + 75 * rise[:, None, None]
+    for power in (np.linspace(60, -40, n), np.linspace(-40, 60, n),
+                  30 * np.cos(np.arange(n))):
+        v = rng.standard_normal((n, 1, dim)) * (2.0 ** power)[:, None, None]
+        f = Filled(rng, 30, 1, 16, dim, 8, 8, rows=[k, v])
+        f.check(q, on(np.arange(30)[None]), on([n]), kind=kind)
