@@ -648,20 +648,6 @@ void attend_kernel(const Attend a) {
             const bool whole = now.token >= span.first &&
                                now.token + 16 <= now.end[0] &&
                                now.token + 32 <= now.end[1];
-            if (!whole) {
-                // tokens that are not seen: a logit of 1 * -inf + 0, no
-                // value.  (Rows never written may hold anything.)
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int32_t t = now.token + 16 * s + 4 * group + i;
-                        const bool seen = (t >= span.first) & (t < now.end[s]);
-                        ks[s][i] = seen ? ks[s][i] : 0x3F80u;
-                        vs[s][i] = seen ? vs[s][i] : 0;
-                        acc[s][i] = seen ? acc[s][i] : -INFINITY;
-                    }
-            }
             float x[2][4];
 #pragma unroll
             for (int s = 0; s < 2; ++s)
@@ -673,6 +659,19 @@ void attend_kernel(const Attend a) {
                         z = __builtin_fmaf(step, kCentreK, z);
                     x[s][i] = __builtin_fmaf(step, acc[s][i], z * q_sum);
                 }
+            if (!whole) {
+                // tokens that are not seen: no weight, no value, whatever
+                // their rows (nobody may have written them) and the query hold
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int32_t t = now.token + 16 * s + 4 * group + i;
+                        const bool seen = (t >= span.first) & (t < now.end[s]);
+                        vs[s][i] = seen ? vs[s][i] : 0;
+                        x[s][i] = seen ? x[s][i] : -INFINITY;
+                    }
+            }
             float big = -INFINITY;
 #pragma unroll
             for (int s = 0; s < 2; ++s)

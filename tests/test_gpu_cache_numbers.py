@@ -139,3 +139,34 @@ def test_logits_that_rise_and_wide_rows_that_fade(kind):
         v = rng.standard_normal((n, 1, dim)) * (2.0 ** power)[:, None, None]
         f = Filled(rng, 30, 1, 16, dim, 8, 8, rows=[k, v])
         f.check(q, on(np.arange(30)[None]), on([n]), kind=kind)
+
+
+# ---- queries ----------------------------------------------------------------
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,longest", [(2, 64), (3, 3000), (64, 700)])
+def test_nothing_visible_with_a_query_that_is_no_number(bad, kind, batch,
+                                                        longest):
+    """A padded place of a batch (length 0, or a table without a page, and
+    whatever its query holds) gives 0 and -inf however the call is shared; a
+    head with visible tokens gives NaN, the others what they are."""
+    say(bad, kind, batch, longest)
+    rng = np.random.default_rng(batch)
+    f = Filled(rng, 40, 2, 16, 64, 8, 4)
+    per = -(-longest // 16)
+    table = rng.integers(0, 40, (batch, per)).astype(np.int32)
+    lengths = rng.integers(1, longest, batch).astype(np.int32)
+    lengths[0], lengths[batch - 1] = 0, longest
+    table[1] = -1
+    q = queries(rng, batch, 4, 64, kind)
+    args = f.cache, torch.from_numpy(table).cuda(), on(lengths)
+    want, want_lse = (host(t) for t in kc.attend(q, *args))
+    q[0], q[1, 2] = bad, bad
+    q[batch - 1, 3, 5] = bad
+    out, lse = (host(t) for t in kc.attend(q, *args))
+    assert (out[:2] == 0).all() and (lse[:2] == -np.inf).all()
+    if batch > 2:
+        assert np.isnan(out[-1, 3]).all() and np.isnan(lse[-1, 3])
+        out[-1, 3], lse[-1, 3] = want[-1, 3], want_lse[-1, 3]
+    assert np.array_equal(out, want) and np.array_equal(lse, want_lse)
