@@ -640,7 +640,7 @@ static bscache_status check_attend(const bscache_pages* cache,
     a->max_len = p->max_len;
     a->window = p->window;
     a->dtype = p->dtype;
-    a->scale2 = p->scale * 1.44269504088896340736f;
+    a->scale = p->scale;
     // units of the longest sequence: its first visible token is taken down
     // to a multiple of 16
     int64_t span = p->max_len;

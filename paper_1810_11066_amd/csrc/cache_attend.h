@@ -78,6 +78,7 @@ constexpr float kBelow = 24.0f;
 constexpr int kMost = 44;
 constexpr int kSmall = -64;
 constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // ---- the row of units ------------------------------------------------------
 
@@ -386,9 +387,9 @@ void attend_kernel(const Attend a) {
     constexpr bool kTwoQ = T == kF32, kCentred = T == kF32;
     constexpr float kCentreK = !kCentred ? 0.0f : KB == 8 ? 128.0f : 8.0f;
     constexpr float kCentreV = !kCentred ? 0.0f : VB == 8 ? 128.0f : 8.0f;
-    // codes over what they are as float16
+    // codes over what they are as float16; of keys, 2^kUnitK
     constexpr float kCode = kCentred ? 1.0f : 0x1p24f;
-    constexpr float kCodeK = KB == 4 ? kCode / 16 : kCentred ? kCode : kCode / 4;
+    constexpr int kUnitK = (kCentred ? 0 : 24) - (KB == 4 ? 4 : kCentred ? 0 : 2);
     constexpr float kCodeV = VB == 8 ? kCode : kCode / 16;
     __shared__ float sm_o[kWaves][16][DP + 4];
     __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
@@ -600,7 +601,7 @@ void attend_kernel(const Attend a) {
             // 2^-e brings the largest into [2^13, 2^14); tiny rows stay below
             const int e = max((int)(f32_bits(top) >> 23), 27) - 127 - 13;
             // (the sign of the scale goes into q: q_scale is not negative)
-            const float down = copysignf(ldexpf(1.0f, -e), a.scale2);
+            const float down = copysignf(ldexpf(1.0f, -e), a.scale);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
@@ -612,8 +613,8 @@ void attend_kernel(const Attend a) {
                     if constexpr (kTwoQ) q_lo[i][j] = (_Float16)(y - (float)hi);
                 }
             // (above 0, so that a masked -inf stays one)
-            q_scale = fmaxf(fabsf(a.scale2) * ldexpf(kCodeK, e), 1e-30f);
-            q_sum = sum * down * (1.0f / kCodeK);
+            q_scale = fmaxf(ldexpf(fabsf(a.scale), e + kUnitK) * kLog2e, 1e-30f);
+            q_sum = sum * down * ldexpf(1.0f, -kUnitK);
         }
 
         f32x4 o[kOwn];

@@ -140,7 +140,7 @@ struct Attend {
     int32_t batch, heads, group;
     int32_t head_tiles;       // tiles of up to 16 query heads of a kv head
     int32_t max_pages, max_len, window, dtype;
-    float scale2;             // scale log2(e)
+    float scale;
     bool whole;               // every pair is one workgroup's
     bool wide;                // of as many waves as a CU holds (whole too)
     int32_t blocks;           // workgroups

@@ -170,3 +170,17 @@ def test_nothing_visible_with_a_query_that_is_no_number(bad, kind, batch,
         assert np.isnan(out[-1, 3]).all() and np.isnan(lse[-1, 3])
         out[-1, 3], lse[-1, 3] = want[-1, 3], want_lse[-1, 3]
     assert np.array_equal(out, want) and np.array_equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("kbits", [8, 4])
+@pytest.mark.parametrize("size", [1e-36, 1e36, 2.5e36])
+def test_queries_far_from_one(kind, kbits, size):
+    """The scale brings the logits back to a few units."""
+    say(kind, kbits, size)
+    rng = np.random.default_rng(11)
+    f = Filled(rng, 8, 1, 32, 64, kbits, 8)
+    q = rounded(rng.uniform(-1, 1, (2, 4, 64)) * size, kind)[1]
+    scale = float(np.float32(4.0 / size)) if size > 1 else 1e35
+    f.check(q, on(np.arange(8).reshape(2, 4)), on([100, 128]), scale=scale,
+            kind=kind)
