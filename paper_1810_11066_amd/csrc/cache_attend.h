@@ -588,16 +588,10 @@ void attend_kernel(const Attend a) {
             for (int i = 0; i < kSteps; ++i) {
                 if (!mine || (group + 4 * (i >> 1)) * 16 >= dim) qx[i].clear();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = qx[i].get(e);
-                    sum += x;
-                    top = fmaxf(top, fabsf(x));
-                }
+                for (int e = 0; e < 8; ++e)
+                    top = fmaxf(top, fabsf(qx[i].get(e)));
             }
             top = over_groups(top, larger);
-            sum = over_groups(sum, add);
-            // an infinity makes the whole head NaN, as a NaN does by itself
-            if (!(top < INFINITY)) sum = NAN;
             // 2^-e brings the largest into [2^13, 2^14); tiny rows stay below
             const int e = max((int)(f32_bits(top) >> 23), 27) - 127 - 13;
             // (the sign of the scale goes into q: q_scale is not negative)
@@ -612,9 +606,17 @@ void attend_kernel(const Attend a) {
                     q_hi[i][j] = hi;
                     if constexpr (kTwoQ) q_lo[i][j] = (_Float16)(y - (float)hi);
                 }
+            // (of what is scaled: a finite row's own sum may be beyond float32)
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += qx[i].get(e) * down;
+            sum = over_groups(sum, add);
+            // an infinity makes the whole head NaN, as a NaN does by itself
+            if (!(top < INFINITY)) sum = NAN;
             // (above 0, so that a masked -inf stays one)
             q_scale = fmaxf(ldexpf(fabsf(a.scale), e + kUnitK) * kLog2e, 1e-30f);
-            q_sum = sum * down * ldexpf(1.0f, -kUnitK);
+            q_sum = ldexpf(sum, -kUnitK);
         }
 
         f32x4 o[kOwn];

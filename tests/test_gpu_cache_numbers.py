@@ -184,3 +184,16 @@ def test_queries_far_from_one(kind, kbits, size):
     scale = float(np.float32(4.0 / size)) if size > 1 else 1e35
     f.check(q, on(np.arange(8).reshape(2, 4)), on([100, 128]), scale=scale,
             kind=kind)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("kbits", [8, 4])
+@pytest.mark.parametrize("size", [2e37, 3e38])
+def test_queries_whose_sum_is_beyond_binary32(kind, kbits, size):
+    """Finite queries of one sign, the sum of which is none."""
+    say(kind, kbits, size)
+    rng = np.random.default_rng(12)
+    f = Filled(rng, 8, 1, 32, 64, kbits, 8)
+    q = rounded(rng.uniform(0.25, 1, (2, 4, 64)) * size, kind)[1]
+    f.check(q, on(np.arange(8).reshape(2, 4)), on([100, 128]),
+            scale=float(np.float32(4.0 / size)), kind=kind)
