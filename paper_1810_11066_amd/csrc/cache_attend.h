@@ -592,8 +592,9 @@ void attend_kernel(const Attend a) {
                     top = fmaxf(top, fabsf(qx[i].get(e)));
             }
             top = over_groups(top, larger);
-            // 2^-e brings the largest into [2^13, 2^14); tiny rows stay below
-            const int e = max((int)(f32_bits(top) >> 23), 27) - 127 - 13;
+            // 2^-e brings the largest into [2^13, 2^14); rows below 2^-114 stay
+            // below
+            const int e = max((int)(f32_bits(top) >> 23), 13) - 127 - 13;
             // (the sign of the scale goes into q: q_scale is not negative)
             const float down = copysignf(ldexpf(1.0f, -e), a.scale);
 #pragma unroll
@@ -614,8 +615,10 @@ void attend_kernel(const Attend a) {
             sum = over_groups(sum, add);
             // an infinity makes the whole head NaN, as a NaN does by itself
             if (!(top < INFINITY)) sum = NAN;
-            // (above 0, so that a masked -inf stays one)
-            q_scale = fmaxf(ldexpf(fabsf(a.scale), e + kUnitK) * kLog2e, 1e-30f);
+            // (above 0, so that a masked -inf stays one, and so little that
+            // nothing finite gets above 2^-20 by it)
+            q_scale =
+                fmaxf(ldexpf(fabsf(a.scale), e + kUnitK) * kLog2e, 0x1p-149f);
             q_sum = ldexpf(sum, -kUnitK);
         }
 

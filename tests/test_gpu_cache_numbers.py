@@ -197,3 +197,24 @@ def test_queries_whose_sum_is_beyond_binary32(kind, kbits, size):
     q = rounded(rng.uniform(0.25, 1, (2, 4, 64)) * size, kind)[1]
     f.check(q, on(np.arange(8).reshape(2, 4)), on([100, 128]),
             scale=float(np.float32(4.0 / size)), kind=kind)
+
+
+def small_scale(kind, scale, size, keys, kbits=8):
+    say(kind, scale, size, keys)
+    rng = np.random.default_rng(12)
+    k = rng.standard_normal((128, 1, 64)) * keys
+    v = rng.standard_normal((128, 1, 64))
+    f = Filled(rng, 8, 1, 16, 64, kbits, 8, rows=[k, v])
+    q = rounded(rng.standard_normal((2, 4, 64)) * size, kind)[1]
+    f.check(q, on(np.arange(8).reshape(2, 4)), on([60, 64]),
+            scale=float(np.float32(scale)), kind=kind)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("scale,size,keys", [
+    (0.0, 1.0, 1e30), (-0.0, 1e-30, 1.0), (1e-32, 1.0, 1e31),
+    (0.1, 1e-30, 1e30), (1e-12, 1e-18, 1e30), (1.0, 1e-37, 1e31)])
+def test_small_scales_of_large_keys(kind, scale, size, keys):
+    """scale * q far below 1 with keys far above: logits of 0 or of a few
+    units."""
+    small_scale(kind, scale, size, keys)
