@@ -129,8 +129,10 @@ bscache_status bscache_read(const bscache_pages *cache, const int32_t *slots,
  *            as 0; they must not change while the call runs;
  *   out:     [batch][heads][dim] of type dtype;
  *   lse:     [batch][heads] float32, or NULL.
- * A sequence without a visible token gets out = 0 and lse = -inf.  A query
- * that holds a NaN or an infinity gives NaN for its head alone.
+ * A sequence without a visible token gets out = 0 and lse = -inf, whatever its
+ * query holds.  Otherwise a query that holds a NaN or an infinity gives NaN for
+ * its head alone.  Logits have to stay within binary32 (times log2 e), and
+ * |scale| times a query's largest element below 2^100.
  * Products are of the exact codes: q enters the matrix units scaled by a power
  * of two as float16 (bfloat16 and float16 values keep their bits but for what
  * lies below 2^-30 of the row's largest; float32 as two float16 of 22 bits

@@ -32,11 +32,11 @@
 //   logit = scale (s (q . c') + z' sum q)
 //   out   = (sum_t w_t c'_t + sum_t p_t z'_t) / sum_t p_t,   w = p s.
 //
-// Roundings: q is scaled by a power of two to below 2^14 and rounded to
-// float16: bfloat16 and float16 values keep all their bits, but for what lies
-// below 2^-30 of the row's largest; float32 queries take a second float16 for
-// the rest (22 bits together), a second MFMA into the same accumulator.  w is
-// two float16 as well, 22 bits.  (One was 2^-12 of w c, whose magnitudes are 3
+// Roundings: q is scaled by a power of two to below 2^14 (2^13 over 4-bit keys)
+// and rounded to float16: bfloat16 and float16 values keep all their bits, but
+// for what lies below 2^-30 of the row's largest; float32 queries take a second
+// float16 for the rest (22 bits together), a second MFMA into the same
+// accumulator.  w is two float16 as well, 22 bits.  (One was 2^-12 of w c, whose magnitudes are 3
 // times the spread of the values where codes are not centred: bfloat16 outputs
 // came out a step off.)
 // Weights and the softmax's sum have references of their own.  p = 2^(logit - m),
@@ -46,9 +46,9 @@
 // to of it, and one that is not, however wide, takes no bits from the others.
 // (2^-10 |z|: z far beyond s is a row of nearly equal values, whose sums 2^k p z
 // would leave float32.  It is looked at only where a sum gets large.)  Both lag
-// by up to 2^8, so w stays below 2^15 and keeps its 22 bits down to 2^-17 of
-// the largest, and is rounded to 2^-31 of it below.  A partial result is the mean
-// of its own tokens, with m and the sum of p.  Everything else is float32.
+// by up to 2^8, so w stays below 2^15; it keeps its 22 bits down to 2^-9 of the
+// largest, and is rounded to 2^-31 of that below.  A partial result is the mean of
+// its own tokens, with m and the sum of p.  Everything else is float32.
 //
 // Sharing: the units of all (sequence, head tile) pairs are numbered in one row
 // of places, and workgroup i of n takes the places [i U / n, (i + 1) U / n):
@@ -387,9 +387,17 @@ void attend_kernel(const Attend a) {
     constexpr bool kTwoQ = T == kF32, kCentred = T == kF32;
     constexpr float kCentreK = !kCentred ? 0.0f : KB == 8 ? 128.0f : 8.0f;
     constexpr float kCentreV = !kCentred ? 0.0f : VB == 8 ? 128.0f : 8.0f;
-    // codes over what they are as float16; of keys, 2^kUnitK
+    // codes over what they are as float16; of keys, and with what the products'
+    // sums are brought down by, 2^kUnitK
     constexpr float kCode = kCentred ? 1.0f : 0x1p24f;
-    constexpr int kUnitK = (kCentred ? 0 : 24) - (KB == 4 ? 4 : kCentred ? 0 : 2);
+    constexpr int kDown = kCentred ? 26 : 0;
+    constexpr int kUnitK =
+        (kCentred ? kDown : 24) - (KB == 4 ? 4 : kCentred ? 0 : 2);
+    // Queries are brought to below 2^(kQ + 1).  With that and kDown the sum of
+    // 256 products with keys of up to 2^126 (1 + 2^-6) stays within float32:
+    // 2^-kUnitK 2^8 2^(kQ + 1) 2^126 is 2^126 and 2^127 for 8- and 4-bit keys of
+    // 16-bit calls, 2^122 and 2^126 for float32.
+    constexpr int kQ = KB == 4 && !kCentred ? 12 : 13;
     constexpr float kCodeV = VB == 8 ? kCode : kCode / 16;
     __shared__ float sm_o[kWaves][16][DP + 4];
     __shared__ float sm_m[kWaves][16], sm_l[kWaves][16];
@@ -592,9 +600,9 @@ void attend_kernel(const Attend a) {
                     top = fmaxf(top, fabsf(qx[i].get(e)));
             }
             top = over_groups(top, larger);
-            // 2^-e brings the largest into [2^13, 2^14); rows below 2^-114 stay
-            // below
-            const int e = max((int)(f32_bits(top) >> 23), 13) - 127 - 13;
+            // 2^-e brings the largest into [2^kQ, 2^(kQ + 1)); rows below 2^-114
+            // may stay below
+            const int e = max((int)(f32_bits(top) >> 23), kQ) - 127 - kQ;
             // (the sign of the scale goes into q: q_scale is not negative)
             const float down = copysignf(ldexpf(1.0f, -e), a.scale);
 #pragma unroll
@@ -663,7 +671,9 @@ void attend_kernel(const Attend a) {
                     float z = offset_of(ks[s][i]);
                     if constexpr (kCentred)
                         z = __builtin_fmaf(step, kCentreK, z);
-                    x[s][i] = __builtin_fmaf(step, acc[s][i], z * q_sum);
+                    const float qc =
+                        kDown ? acc[s][i] * ldexpf(1.0f, -kDown) : acc[s][i];
+                    x[s][i] = __builtin_fmaf(step, qc, z * q_sum);
                 }
             if (!whole) {
                 // tokens that are not seen: no weight, no value, whatever

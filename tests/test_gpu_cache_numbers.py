@@ -218,3 +218,36 @@ def test_small_scales_of_large_keys(kind, scale, size, keys):
     """scale * q far below 1 with keys far above: logits of 0 or of a few
     units."""
     small_scale(kind, scale, size, keys)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("kbits", [8, 4])
+@pytest.mark.parametrize("scale,size,keys", [
+    (0.0, 1e30, 1e36), (1e-20, 1e-18, 1e37), (0.1, 1e-35, 1e35)])
+def test_keys_far_from_one(kind, kbits, scale, size, keys):
+    """The same of keys next to the largest that a cache keeps."""
+    small_scale(kind, scale, size, keys, kbits)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("kbits", [8, 4])
+def test_keys_at_the_ends(kind, kbits):
+    """Keys up to 2^126 (what infinities are kept as) in every channel, with
+    queries of one sign, and a scale that brings the logits back."""
+    say(kind, kbits)
+    rng = np.random.default_rng(13)
+    n, dim = 64, 256
+    k = rng.standard_normal((n, 1, dim)) * 1e37
+    k[3, 0, 1:] = np.inf
+    k[3, 0, 0] = -np.inf
+    k[9] = -np.inf
+    k[9, 0, 77] = np.inf
+    k[11] = np.inf
+    v = rng.standard_normal((n, 1, dim))
+    with np.errstate(all="ignore"):
+        f = Filled(rng, 4, 1, 16, dim, kbits, 8, rows=[k, v])
+    # (the largest logit: 256 * 2^126 * scale * q = 20)
+    q = np.ones((1, 2, dim)) * np.array([255 / 128, -1.5])[None, :, None] / 1024
+    q[0, :, 0] *= -1                # as the key's: nothing cancels
+    q = rounded(q, kind)[1]
+    f.check(q, on([[0, 1, 2, 3]]), on([n]), scale=20 * 2.0 ** -125, kind=kind)
