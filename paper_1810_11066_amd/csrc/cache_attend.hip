@@ -147,7 +147,7 @@ void plan_attend(Attend& a, int64_t tokens) {
     a.few = pairs >= cus || heads * (a.c.dim >> 2) * units <= kDeep * kThreads
                 ? heads : 1;
     const int64_t parts = 2 * a.blocks * part_bytes(a.c.dim);
-    a.workspace = a.whole ? 0 : parts + 8 * pairs;
+    a.workspace = a.whole || pairs == 0 ? 0 : parts + 8 * pairs;
 }
 
 hipError_t launch_attend(const Attend& a, hipStream_t st) {
