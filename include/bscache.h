@@ -95,7 +95,8 @@ typedef struct {
  * Errors: INVALID_ARG for NULL/misaligned pointers, sizes < 1 (tokens < 0),
  * strides < kv_heads * dim or not of whole 16 bytes, an unknown dtype, buffers
  * that overlap; UNSUPPORTED for sizes beyond those of bscache_pages and for
- * calls of more than 2^31 - 1 rows. */
+ * calls of more than 2^31 - 1 rows (keys' and values'), or of 2^33 / L and more
+ * with L = dim / 8 up to a power of two (a launch has 2^32 lanes). */
 bscache_status bscache_write(const bscache_pages *cache, const void *k,
                              const void *v, int64_t k_stride,
                              int64_t v_stride, bscache_dtype dtype,
@@ -145,8 +146,10 @@ bscache_status bscache_read(const bscache_pages *cache, const int32_t *slots,
  * < 1, heads not a multiple of kv_heads, max_len beyond max_pages *
  * page_tokens, window < 0, a scale that is not finite, q_stride < heads * dim
  * or not of whole 16 bytes, a workspace that is too small, buffers that
- * overlap; UNSUPPORTED as bscache_pages and for problems of more than 2^31 - 1
- * tiles of 64 tokens or rows of out. */
+ * overlap; UNSUPPORTED as bscache_pages and for problems of 2^24 or more pairs
+ * of a sequence and up to 16 query heads of a key-value head, of more than 2^30
+ * units of 128 tokens of them (8 added for each), or of more than 2^31 - 1 rows
+ * of out. */
 typedef struct {
     int64_t q_stride;
     int32_t batch, heads;

@@ -11,8 +11,6 @@
 namespace bscache {
 namespace {
 
-constexpr int kBlock = 256;
-
 // ---------------------------------------------------------------------------
 // Rows.  LPR lanes (a power of two, at least dim / 8) share a row, 8
 // consecutive channels each, so a wave has 64 / LPR rows at a time: rows of
@@ -348,12 +346,17 @@ struct Read {
     }
 };
 
+int lanes_of_row(const Pages& c) {
+    int lpr = 2;
+    while (lpr * 8 < c.dim) lpr *= 2;
+    return lpr;
+}
+
 // Lanes of a row, groups of a wave and grid of a call: two groups once the waves
 // of single ones are more than `full` on a SIMD.
 RowsGrid rows_grid(const Pages& c, int64_t tokens, int full, int* lpr,
                    int* steps) {
-    *lpr = 2;
-    while (*lpr * 8 < c.dim) *lpr *= 2;
+    *lpr = lanes_of_row(c);
     const int rows = 64 / *lpr;
     const int64_t pairs = 2 * (int64_t)c.kv_heads;
     *steps = (tokens + rows - 1) / rows * pairs >
@@ -382,6 +385,13 @@ int device_cus() {
         __atomic_store_n(&cus[dev], n, __ATOMIC_RELAXED);
     }
     return n;
+}
+
+bool rows_fit(const Pages& c, int64_t tokens) {
+    // (so many come two groups to a wave)
+    const int64_t per = 2 * (64 / lanes_of_row(c));
+    return (tokens + per - 1) / per * 2 * c.kv_heads <=
+           kBlock / 64 * kMostBlocks;
 }
 
 hipError_t launch_write(const Pages& c, const void* k, const void* v,
@@ -535,10 +545,13 @@ uint64_t strided_bytes(int64_t rows, int64_t stride, int64_t row, int dtype) {
     return rows < 1 ? 0 : ((uint64_t)(rows - 1) * stride + row) * size_of(dtype);
 }
 
-bscache_status check_tokens(int64_t tokens, int kv_heads) {
+bscache_status check_tokens(int64_t tokens, const bscache::Pages& c) {
     if (tokens < 0) return fail(BSCACHE_ERR_INVALID_ARG, "tokens < 0");
-    if (tokens > INT32_MAX / (2 * (int64_t)kv_heads))
-        return fail(BSCACHE_ERR_UNSUPPORTED, "more than 2^31 - 1 rows");
+    if (tokens > INT32_MAX / (2 * (int64_t)c.kv_heads) ||
+        !bscache::rows_fit(c, tokens))
+        return fail(BSCACHE_ERR_UNSUPPORTED,
+                    "%lld tokens have more rows than a launch has lanes for",
+                    (long long)tokens);
     return BSCACHE_OK;
 }
 
@@ -563,7 +576,7 @@ bscache_status bscache_write(const bscache_pages* cache, const void* k,
     if ((st = check_ptr(k, "k")) != BSCACHE_OK) return st;
     if ((st = check_ptr(v, "v")) != BSCACHE_OK) return st;
     if ((st = check_ptr(slots, "slots")) != BSCACHE_OK) return st;
-    if ((st = check_tokens(tokens, c.kv_heads)) != BSCACHE_OK) return st;
+    if ((st = check_tokens(tokens, c)) != BSCACHE_OK) return st;
     const int64_t row = (int64_t)c.kv_heads * c.dim;
     if ((st = check_stride(k_stride, row, dtype, "k_stride")) != BSCACHE_OK)
         return st;
@@ -592,7 +605,7 @@ bscache_status bscache_read(const bscache_pages* cache, const int32_t* slots,
     if ((st = check_ptr(slots, "slots")) != BSCACHE_OK) return st;
     if ((st = check_ptr(k, "k")) != BSCACHE_OK) return st;
     if ((st = check_ptr(v, "v")) != BSCACHE_OK) return st;
-    if ((st = check_tokens(tokens, c.kv_heads)) != BSCACHE_OK) return st;
+    if ((st = check_tokens(tokens, c)) != BSCACHE_OK) return st;
     if (tokens == 0) return ok();
     in[4] = {slots, (uint64_t)tokens * 4, "slots"};
     const int64_t row = (int64_t)c.kv_heads * c.dim;
@@ -648,10 +661,14 @@ static bscache_status check_attend(const bscache_pages* cache,
         span = (int64_t)p->window + 15;
     const int64_t units = (span + bscache::kUnit - 1) / bscache::kUnit;
     const int64_t pairs = (int64_t)a->c.kv_heads * a->head_tiles;
-    if ((int64_t)p->batch * pairs > INT32_MAX / (2 * (units + 8)) ||
+    if (p->batch * pairs > bscache::kMostBlocks)
+        return fail(BSCACHE_ERR_UNSUPPORTED,
+                    "%lld pairs of a sequence and up to 16 query heads: 2^24 or "
+                    "more", (long long)(p->batch * pairs));
+    if (p->batch * pairs > INT32_MAX / (2 * (units + 8)) ||
         (int64_t)p->batch * p->heads > INT32_MAX)
         return fail(BSCACHE_ERR_UNSUPPORTED,
-                    "more than 2^31 - 1 tiles of 64 tokens, or rows");
+                    "more than 2^30 units of 128 tokens, or 2^31 - 1 rows");
     bscache::plan_attend(*a, span);
     *workspace = a->workspace;
     return BSCACHE_OK;

@@ -115,10 +115,18 @@ hipError_t launch(void (*fn)(P...), uint32_t blocks, uint32_t threads,
                            0, st);
 }
 
+// Workgroups of kBlock that a launch may have: the grid of all threads has 32
+// bits, and so has a thread's number.
+constexpr int kBlock = 256;
+constexpr int64_t kMostBlocks = ((int64_t)1 << 32) / kBlock - 1;
+
 // ---- launchers (each returns hipSuccess or the launch error) ---------------
 
 // Compute units of the current device (cached per device).
 int device_cus();
+
+// Whether write and read launch so many tokens' rows at once.
+bool rows_fit(const Pages& c, int64_t tokens);
 
 hipError_t launch_write(const Pages& c, const void* k, const void* v,
                         int64_t k_stride, int64_t v_stride, int dtype,

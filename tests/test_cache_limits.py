@@ -1,10 +1,11 @@
 """libbscache.so at the ends of what it takes (no GPU): every call below fails
 validation, has nothing to do or is described only."""
-import ctypes
+import pytest
 
 from paper_1810_11066_amd import cache as kc
-from tests.test_cache_abi import (A, B, C, D, E, INVALID, attend, lib, pages,
-                                  params, workspace)
+from tests.test_cache_abi import (A, B, C, D, E, INVALID, KC, UNSUPPORTED,
+                                  attend, lib, pages, params, read, workspace,
+                                  write)
 
 assert lib      # (a fixture)
 
@@ -17,3 +18,39 @@ def test_an_empty_batch_needs_no_workspace(lib):
     assert lib.bscache_attend(pages(), none, A, B, C, D, E, None, 0,
                               None) == kc.OK
     assert attend(lib, p=one, space=0) == INVALID
+
+
+@pytest.mark.parametrize("dim,lanes", [(256, 32), (144, 32), (128, 16),
+                                       (80, 16), (64, 8), (16, 2)])
+@pytest.mark.parametrize("heads", [1, 8])
+def test_rows_of_a_launch(lib, dim, lanes, heads):
+    """As many as its lanes, two rows to a lane, and no more than 2^31 - 1: what
+    fits gets to the check of overlaps (and is refused there)."""
+    cache = pages(heads=heads, dim=dim)
+    most = min((2 ** 31 - 1) // (2 * heads),
+               (2 ** 26 - 4) // (2 * heads) * (128 // lanes))
+    assert abs(most * 2 * heads * lanes / min(2 ** 33, 2 ** 31 * lanes) - 1) \
+        < 1e-6
+    stride = heads * dim
+    for tokens, status in ((most, INVALID), (most + 1, UNSUPPORTED)):
+        assert read(lib, cache, tokens=tokens, v=KC) == status
+        assert write(lib, cache, tokens=tokens, ks=stride, vs=stride,
+                     slots=KC) == status
+    assert b"rows" in lib.bscache_last_error()
+
+
+def test_pairs_of_a_launch(lib):
+    """Whole pairs are a workgroup each, and so are those of the join: 2^24 of a
+    sequence and up to 16 heads of a key-value head are too many."""
+    def status(batch, kv_heads, group, length):
+        heads = kv_heads * group
+        return workspace(lib, pages(heads=kv_heads), params(
+            batch=batch, heads=heads, stride=64 * heads, max_len=length,
+            max_pages=100))[0]
+    assert status(2 ** 22 - 1, 4, 16, 512) == kc.OK
+    assert status(2 ** 22, 4, 16, 512) == UNSUPPORTED
+    assert status(2 ** 21 - 1, 4, 17, 16) == kc.OK          # two tiles each
+    assert status(2 ** 21, 4, 17, 16) == UNSUPPORTED
+    assert status(2 ** 24 - 1, 1, 1, 1024) == kc.OK
+    assert status(2 ** 24, 1, 1, 1024) == UNSUPPORTED
+    assert b"pairs" in lib.bscache_last_error()
