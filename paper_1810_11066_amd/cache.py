@@ -354,7 +354,7 @@ def attend(q: torch.Tensor, cache, table: torch.Tensor, lengths: torch.Tensor,
     if batch == 0:
         return out, lse
     if max_len is None:
-        max_len = max_pages * page_tokens
+        max_len = min(max_pages * page_tokens, 2 ** 31 - 1)
     need = _workspace(device, cache[0].shape[0], kv_heads, page_tokens, dim,
                       batch, heads, max_pages, max_len, window, kind)
     space = torch.empty(need, dtype=torch.uint8, device=q.device) if need \

@@ -89,8 +89,7 @@ struct Span {
     __device__ __forceinline__ int32_t start() const { return first & ~15; }
     // a sequence without tokens has one unit: somebody writes its zeros
     __device__ __forceinline__ int32_t units(int32_t tokens = kUnit) const {
-        const int32_t n = (length - start() + tokens - 1) / tokens;
-        return n > 1 ? n : 1;
+        return (length - start() - 1) / tokens + 1;
     }
 };
 __device__ __forceinline__ int32_t length_of(const Attend& a, int32_t b) {
@@ -369,9 +368,9 @@ __device__ __forceinline__ float rounded(float x) {
 // token, and the end of its visible tokens (0 where its page is none of the
 // cache).  Half a tile never leaves a page (pages are multiples of 16 tokens).
 struct Tile {
-    int32_t token;          // first token
+    uint32_t token;         // first token (a unit may end beyond 2^31)
     int64_t row[2];
-    int32_t end[2];
+    uint32_t end[2];
 };
 
 template <int DP, int KB, int VB, int T, bool WIDE>
@@ -514,11 +513,11 @@ void attend_kernel(const Attend a) {
         const int64_t table = (int64_t)now_seq * a.max_pages;
         auto find = [&](int32_t c) {
             Tile t;
-            t.token = span.start() + c * kStep + wave * 32;
+            t.token = (uint32_t)span.start() + (uint32_t)c * kStep + wave * 32;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const int32_t at = t.token + 16 * s;
-                const bool in = at < span.length && c < c1;
+                const uint32_t at = t.token + 16 * s;
+                const bool in = at < (uint32_t)span.length && c < c1;
                 const uint32_t p = in ? a.c.by_page.div(at) : 0;
                 const uint32_t page = uniform_load(a.table, table + p);
                 const bool there = in && page < a.c.pages;
@@ -659,7 +658,8 @@ void attend_kernel(const Attend a) {
             if (more) load_keys(next);
 
             // ---- softmax
-            const bool whole = now.token >= span.first &&
+            const uint32_t first = span.first;
+            const bool whole = now.token >= first &&
                                now.token + 16 <= now.end[0] &&
                                now.token + 32 <= now.end[1];
             float x[2][4];
@@ -682,8 +682,8 @@ void attend_kernel(const Attend a) {
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int32_t t = now.token + 16 * s + 4 * group + i;
-                        const bool seen = (t >= span.first) & (t < now.end[s]);
+                        const uint32_t t = now.token + 16 * s + 4 * group + i;
+                        const bool seen = (t >= first) & (t < now.end[s]);
                         vs[s][i] = seen ? vs[s][i] : 0;
                         x[s][i] = seen ? x[s][i] : -INFINITY;
                     }
