@@ -20,6 +20,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import os
 import struct
 import threading
@@ -99,14 +100,26 @@ def load_library():
         return lib
 
 
+def _refuse_numbers(values, e):
+    raise ValueError("batch, heads, max_pages, max_len and window must be "
+                     "32-bit integers, scale a binary32 number (got %s)"
+                     % (values,)) from e
+
+
 def _params(*values) -> bytes:
     """Packed bscache_attend_params."""
     try:
         return _PARAMS.pack(*values)
     except (struct.error, OverflowError) as e:
-        raise ValueError("batch, heads, max_pages, max_len and window must be "
-                         "32-bit integers, scale a binary32 number (got %s)"
-                         % (values[1:6] + values[7:],)) from e
+        _refuse_numbers(values[1:6] + values[7:], e)
+
+
+def _integer(x) -> int:
+    """An integer of any kind (a tensor's, say, as it is now) as an int."""
+    try:
+        return operator.index(x)
+    except TypeError as e:
+        _refuse_numbers(x, e)
 
 
 def _check(status: int):
@@ -355,6 +368,10 @@ def attend(q: torch.Tensor, cache, table: torch.Tensor, lengths: torch.Tensor,
         return out, lse
     if max_len is None:
         max_len = min(max_pages * page_tokens, 2 ** 31 - 1)
+    elif type(max_len) is not int:
+        max_len = _integer(max_len)
+    if type(window) is not int:
+        window = _integer(window)
     need = _workspace(device, cache[0].shape[0], kv_heads, page_tokens, dim,
                       batch, heads, max_pages, max_len, window, kind)
     space = torch.empty(need, dtype=torch.uint8, device=q.device) if need \
