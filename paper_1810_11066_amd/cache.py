@@ -3,8 +3,8 @@ cache of 8- or 4-bit codes and the attention that reads it.
 
 ``write``, ``read`` and ``attend`` take torch tensors on the GPU, check them,
 allocate the outputs (and the workspace) with torch and call the C entry point
-on the current stream of the tensors' device, or on ``stream`` (which then
-owns the outputs' memory, as under ``torch.cuda.stream``).  Everything is
+on the current stream of the tensors' device, or on ``stream`` of that device
+(which then owns the outputs' memory, as under ``torch.cuda.stream``).  Everything is
 computed by the library's HIP kernels; there is no host fallback.
 
 A cache is four tensors (``empty`` allocates them; any tuple of four does):
@@ -141,6 +141,16 @@ def _stream(device: int) -> int:
     if _raw_stream is None:
         return torch.cuda.current_stream(device).cuda_stream
     return _raw_stream(device)
+
+
+def _under(stream, cache):
+    """The context in which `stream` is the current one, of the cache's device."""
+    t = cache[0]
+    device = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if device >= 0 and stream.device.index != device:
+        raise ValueError("the stream is of %s, the cache on cuda:%d"
+                         % (stream.device, device))
+    return torch.cuda.stream(stream)
 
 
 def _call(device: int, fn, *args) -> None:
@@ -291,7 +301,7 @@ def write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache,
     apart (slices of a projection's output).  slots: [tokens] int32; a token
     whose slot is outside the cache (-1) is left out; no slot twice."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _under(stream, cache):
             return write(k, v, slots, cache)
     if not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError("k must be a [tokens, kv_heads, dim] tensor")
@@ -319,7 +329,7 @@ def read(slots: torch.Tensor, cache, dim: int, dtype=torch.float32,
     [tokens, kv_heads, dim] of `dtype` (bscache_read); zeros for a slot
     outside the cache."""
     if stream is not None:
-        with torch.cuda.stream(stream):     # the outputs are this stream's
+        with _under(stream, cache):         # the outputs are this stream's
             return read(slots, cache, dim, dtype)
     kind = _DTYPES.get(dtype)
     if kind is None:
@@ -351,7 +361,7 @@ def attend(q: torch.Tensor, cache, table: torch.Tensor, lengths: torch.Tensor,
     saves workgroups that find nothing to do.  out is like q, lse float32
     [batch, heads]; a sequence without visible tokens gets 0 and -inf."""
     if stream is not None:
-        with torch.cuda.stream(stream):     # outputs and workspace too
+        with _under(stream, cache):         # outputs and workspace too
             return attend(q, cache, table, lengths, scale, window, max_len)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a [batch, heads, dim] tensor")

@@ -1,6 +1,9 @@
 """libbscache.so at the ends of what it takes (no GPU): every call below fails
 validation, has nothing to do or is described only."""
+import types
+
 import pytest
+import torch
 
 from paper_1810_11066_amd import cache as kc
 from tests.test_cache_abi import (A, B, C, D, E, INVALID, KC, UNSUPPORTED,
@@ -54,3 +57,23 @@ def test_pairs_of_a_launch(lib):
     assert status(2 ** 24 - 1, 1, 1, 1024) == kc.OK
     assert status(2 ** 24, 1, 1, 1024) == UNSUPPORTED
     assert b"pairs" in lib.bscache_last_error()
+
+
+def test_a_stream_of_another_device_is_refused():
+    """Its handle would not be used: the call would go to the current stream of
+    the cache's device."""
+    class OnSecond(torch.Tensor):
+        is_cuda = True
+
+        def get_device(self):
+            return 1
+    cache = kc.Pages(*(torch.zeros((2, 1, 16, n), dtype=t).as_subclass(
+        OnSecond) for n, t in ((64, torch.uint8), (2, torch.bfloat16)) * 2))
+    x, slots = torch.zeros((3, 1, 64)), torch.zeros(3, dtype=torch.int32)
+    stream = types.SimpleNamespace(device=torch.device("cuda", 0))
+    for call in (lambda: kc.write(x, x, slots, cache, stream=stream),
+                 lambda: kc.read(slots, cache, 64, stream=stream),
+                 lambda: kc.attend(x, cache, slots.view(3, 1), slots,
+                                   stream=stream)):
+        with pytest.raises(ValueError, match="cuda:0, the cache on cuda:1"):
+            call()
