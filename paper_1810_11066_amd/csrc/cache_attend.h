@@ -73,9 +73,9 @@ namespace bscache {
 constexpr float kNone = -3.0e38f;       // reference of no logits
 // The reference m is so far below the running maximum.
 constexpr float kBelow = 24.0f;
-// k of the first tokens: the largest p is above 2^(kBelow - 1), a step at least
-// 2^-60.
-constexpr int kMost = 44;
+// k of the first tokens: the largest p is 2^(kBelow - 1) and more (where binary32
+// has no whole numbers, 1 and more), a step at least 2^-60.
+constexpr int kMost = 68;
 constexpr int kSmall = -64;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -711,11 +711,22 @@ void attend_kernel(const Attend a) {
             }
             float p[8], w[8], z_next;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 8; ++i)
                 p[i] = __builtin_amdgcn_exp2f(
                     __builtin_fmaf(x[i >> 2][i & 3], q_scale, -m));
-                sum_p += p[i];
+            // where binary32's steps are not far below 1, the logits as they are
+            // rounded, as the maximum is
+            const bool far = !(fabsf(m) < 0x1p20f);
+            if (__any(far)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float y = __builtin_amdgcn_exp2f(
+                        x[i >> 2][i & 3] * q_scale - m);
+                    p[i] = far ? y : p[i];
+                }
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum_p += p[i];
             auto offset = [&](int i) {
                 const float z = offset_of(vs[i >> 2][i & 3]);
                 return kCentred ? __builtin_fmaf(step_of(vs[i >> 2][i & 3]),
@@ -877,7 +888,7 @@ void attend_kernel(const Attend a) {
                 *reinterpret_cast<f32x4*>(part + h * dim + d) = r;
                 if (d == 0)
                     *reinterpret_cast<float2*>(part + 16 * dim + 2 * h) =
-                        make_float2(top - (float)kSmall, ldexpf(l, kSmall));
+                        make_float2(top, ldexpf(l, kSmall));
             }
         }
         if (last) break;

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a) {
             }
         }
         if (on && mine == 0)
-            finish(a, a.dtype, row0 + h, d, m, l, mean(r, l));
+            finish(a, a.dtype, row0 + h, d, m, ldexpf(l, -kSmall), mean(r, l));
     }
 }
 

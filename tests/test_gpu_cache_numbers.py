@@ -251,3 +251,34 @@ def test_keys_at_the_ends(kind, kbits):
     q[0, :, 0] *= -1                # as the key's: nothing cancels
     q = rounded(q, kind)[1]
     f.check(q, on([[0, 1, 2, 3]]), on([n]), scale=20 * 2.0 ** -125, kind=kind)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+@pytest.mark.parametrize("scale", [1 + i / 64 for i in range(24)])
+def test_logits_that_binary32_has_in_steps_of_128(kind, scale):
+    """Logits of 2^30 and the next number in binary32: only the largest count.
+    (Two thirds of a shared sequence hold keys of 1, the rest keys of 1 + 2^-23,
+    every product and sum exact.)"""
+    say(kind, scale)
+    rng = np.random.default_rng(14)
+    n, dim, first = 3000, 64, 2000
+    f = Filled(rng, 188, 1, 16, dim, 8, 8)
+    kc_, ks = f.cache.k_codes, f.cache.k_steps
+    kc_.zero_()
+    kc_.view(-1, dim)[first:] = 1
+    ks[..., 0], ks[..., 1] = 2.0 ** -23, 1.0
+    q = torch.full((1, 1, dim), 2.0 ** 10, dtype=DTYPE[kind], device="cuda")
+    assert " shared " in kc.describe(188, 1, 16, dim, 1, 1, 188 * 16,
+                                     dtype=DTYPE[kind])
+    out, lse = kc.attend(q, f.cache, on(np.arange(188)[None]), on([n]),
+                         scale=scale * 2.0 ** 14)
+    cv, sv, zv = (t[first:n, 0] for t in f.held[1])
+    v = zv[:, None] + sv[:, None] * cv.astype(np.float64)
+    # (sums of 1000 tokens: ref.error_terms)
+    _, by_weight, by_sum = ref.error_terms(kind, dim, n - first)
+    tol = ref.STEP[kind] * np.abs(v.mean(0)) + \
+        np.abs(v).mean(0) * (by_weight + by_sum) * 3
+    assert (np.abs(host(out)[0, 0] - v.mean(0)) <= tol).all()
+    # half a step of the logit, and of its product with log2 e and ln 2
+    want = scale * 2.0 ** 30 * (1 + 2.0 ** -23)
+    assert abs(float(lse) - want) <= 4 * 2.0 ** -24 * want
