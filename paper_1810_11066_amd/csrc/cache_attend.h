@@ -695,8 +695,11 @@ void attend_kernel(const Attend a) {
                 for (int i = 0; i < 4; ++i) big = fmaxf(big, x[s][i]);
             big *= q_scale;
             if (__any(big > m + (kBelow + 8.0f))) {
+                // (of the heads that need it: the others stay as they would
+                // without this one beside them)
+                const float all = over_groups(big, larger);
                 const float m_new =
-                    fmaxf(m, ceilf(over_groups(big, larger)) - kBelow);
+                    all > m + (kBelow + 8.0f) ? fmaxf(m, ceilf(all) - kBelow) : m;
                 // (from kNone: more than any exponent)
                 const int up = (int)fminf(m_new - m, 2000.0f);
                 // what p falls by the weights keep, as far as k goes
@@ -746,7 +749,9 @@ void attend_kernel(const Attend a) {
             float w_big = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w_big = fmaxf(w_big, w[i]);
-            if (__any(w_big > 0x1p15f || !(fabsf(z_next) <= 0x1p100f))) {
+            const bool large = w_big > 0x1p15f || !(fabsf(z_next) <= 0x1p100f);
+            if (__any(large)) {
+                const bool its = over_groups(large ? 1.0f : 0.0f, larger) > 0.0f;
                 float most = 0.0f;          // of 2^-64 p max(s, 2^-10 |z|)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -760,7 +765,7 @@ void attend_kernel(const Attend a) {
                 const int e_z =
                     (int)(f32_bits(over_groups(fabsf(sum_z), larger)) >> 23) -
                     126;
-                const int k_new = min(k, min(7 - e, k + 40 - e_z));
+                const int k_new = its ? min(k, min(7 - e, k + 40 - e_z)) : k;
                 const float f = ldexpf(1.0f, k_new - k);
                 sum_z *= f;
 #pragma unroll

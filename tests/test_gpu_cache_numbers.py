@@ -282,3 +282,47 @@ def test_logits_that_binary32_has_in_steps_of_128(kind, scale):
     # half a step of the logit, and of its product with log2 e and ln 2
     want = scale * 2.0 ** 30 * (1 + 2.0 ** -23)
     assert abs(float(lse) - want) <= 4 * 2.0 ** -24 * want
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n", [200, 3000])
+def test_heads_know_nothing_of_each_other(kind, n):
+    """A head's bits are the same whatever the other heads of its tile hold;
+    the rows' sizes and the logits are far enough apart for references to move
+    all the time."""
+    say(kind, n)
+    rng = np.random.default_rng(n)
+    dim, pages = 64, -(-n // 16)
+    k = rng.standard_normal((16 * pages, 1, dim)) * 4
+    v = rng.standard_normal((16 * pages, 1, dim)) * \
+        2.0 ** rng.uniform(-30, 10, (16 * pages, 1, 1))
+    f = Filled(rng, pages, 1, 16, dim, 8, 8, rows=[k, v])
+    q = queries(rng, 1, 12, dim, kind)
+    args = f.cache, on(np.arange(pages)[None]), on([n])
+    out, lse = f.check(q, *args[1:], kind=kind)
+    for other in (0.0, 1e3, float("nan"), float("inf")):
+        for keep in (0, 7, 11):
+            p = torch.full_like(q, other)
+            p[:, keep] = q[:, keep]
+            got, got_lse = (host(t) for t in kc.attend(p, *args))
+            assert np.array_equal(got[:, keep], out[:, keep]), (other, keep)
+            assert np.array_equal(got_lse[:, keep], lse[:, keep])
+
+
+def test_small_weights_beside_a_head_that_is_no_number():
+    """Weights 2^-24 of a wave's largest, which came within what a reference may
+    lag: what float16 holds of them does not depend on another head."""
+    rng = np.random.default_rng(15)
+    n, dim = 500, 64
+    k = rng.standard_normal((512, 1, dim)) * 0.01
+    v = rng.standard_normal((512, 1, dim)) * 2.0 ** -16
+    v[0], v[128] = rng.standard_normal((2, 1, dim)) * [[[1.0]], [[180.0]]]
+    f = Filled(rng, 32, 1, 16, dim, 8, 8, rows=[k, v])
+    q = queries(rng, 1, 12, dim, "f32")
+    args = f.cache, on(np.arange(32)[None]), on([n])
+    out, lse = f.check(q, *args[1:], kind="f32")
+    q[0, 5] = float("nan")
+    got, got_lse = (host(t) for t in kc.attend(q, *args))
+    rest = np.arange(12) != 5
+    assert np.array_equal(got[:, rest], out[:, rest])
+    assert np.array_equal(got_lse[:, rest], lse[:, rest])
