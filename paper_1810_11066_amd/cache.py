@@ -399,10 +399,21 @@ def describe(pages: int, kv_heads: int, page_tokens: int, dim: int,
              batch: int, heads: int, max_len: int, kbits: int = 8,
              vbits: int = 8, window: int = 0, dtype=torch.bfloat16) -> str:
     """Kernel and launch that attend would use for these sizes (host only)."""
+    kind = _DTYPES.get(dtype)
+    if kind is None:
+        raise TypeError("dtype must be float32, float16 or bfloat16 (got %s)"
+                        % (dtype,))
+    numbers = pages, kv_heads, page_tokens, dim, kbits, vbits
+    try:
+        cache = _PAGES.pack(*numbers, 0, 0, 0, 0)
+    except struct.error as e:
+        raise ValueError("pages must be a 64-bit integer, kv_heads, page_tokens, "
+                         "dim, kbits and vbits 32-bit ones (got %s)"
+                         % (numbers,)) from e
+    # (no page holds a token where page_tokens is none: refused below)
+    max_pages = -(-max_len // page_tokens) if page_tokens else 1
     buf = ctypes.create_string_buffer(256)
     _check(load_library().bscache_attend_describe(
-        _PAGES.pack(pages, kv_heads, page_tokens, dim, kbits, vbits, 0, 0, 0,
-                    0),
-        _params(heads * dim, batch, heads, -(-max_len // page_tokens), max_len,
-                window, _DTYPES[dtype], 1.0), buf, 256))
+        cache, _params(heads * dim, batch, heads, max_pages, max_len, window,
+                       kind, 1.0), buf, 256))
     return buf.value.decode()

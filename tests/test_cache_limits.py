@@ -77,3 +77,18 @@ def test_a_stream_of_another_device_is_refused():
                                    stream=stream)):
         with pytest.raises(ValueError, match="cuda:0, the cache on cuda:1"):
             call()
+
+
+def test_describe_refuses_as_a_call_does():
+    sizes = dict(pages=4, kv_heads=1, page_tokens=16, dim=64, batch=1, heads=4,
+                 max_len=16)
+    assert kc.describe(**sizes).startswith("attend_kernel<64")
+    for change, error in ((dict(page_tokens=0), kc.CacheError),
+                          (dict(page_tokens=-16), kc.CacheError),
+                          (dict(dim=24), kc.CacheError),
+                          (dict(dtype=torch.float64), TypeError),
+                          (dict(kv_heads=1 << 31), ValueError),
+                          (dict(pages=1 << 63), ValueError),
+                          (dict(dim=64.0), ValueError)):
+        with pytest.raises(error):
+            kc.describe(**{**sizes, **change})
