@@ -92,3 +92,18 @@ def test_describe_refuses_as_a_call_does():
                           (dict(dim=64.0), ValueError)):
         with pytest.raises(error):
             kc.describe(**{**sizes, **change})
+
+
+@pytest.mark.parametrize("dim,dtype,ways", [
+    (64, torch.bfloat16, "whole shared wide wide whole shared whole shared"),
+    (128, torch.float16, "whole shared wide wide whole whole whole shared"),
+    (256, torch.bfloat16, "whole shared wide shared whole whole whole shared"),
+    (96, torch.float32, "whole shared wide shared whole whole whole shared")])
+def test_ways_at_the_bounds_of_the_plan(dim, dtype, ways):
+    """Those that test_gpu_cache.test_attend_on_both_sides_of_the_plan is made
+    for (256 compute units)."""
+    calls = ((1, 500), (1, 700), (12, 700), (20, 1500), (50, 1000), (60, 1100),
+             (70, 2000), (70, 2100))
+    assert [kc.describe(200, 8, 32, dim, batch, 16, longest, 8, 4,
+                        dtype=dtype).split()[4]
+            for batch, longest in calls] == ways.split()
