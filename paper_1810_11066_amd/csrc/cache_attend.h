@@ -41,7 +41,8 @@
 // came out a step off.)
 // Weights and the softmax's sum have references of their own.  p = 2^(logit - m),
 // m 24 below the running maximum in whole numbers, so that what float32 drops is
-// 2^-150 of the largest and less.  w = 2^k p s, with k such that the largest
+// 2^-150 of the largest and less (a wave's only token has p = 1, and its value
+// comes out as it is).  w = 2^k p s, with k such that the largest
 // p max(s, 2^-10 |z|) so far makes 2^6 to 2^7: a row counts by what is attended
 // to of it, and one that is not, however wide, takes no bits from the others.
 // (2^-10 |z|: z far beyond s is a row of nearly equal values, whose sums 2^k p z
@@ -632,7 +633,7 @@ void attend_kernel(const Attend a) {
         f32x4 o[kOwn];
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) o[j] = f32x4{0, 0, 0, 0};
-        float m = kNone;            // reference of p, a whole number
+        float m = kNone;            // reference of p
         int k = kMost;              // of the weights: w = 2^k p s
         float sum_p = 0.0f;
         float sum_z = 0.0f;         // of 2^k p z
@@ -675,9 +676,18 @@ void attend_kernel(const Attend a) {
                         kDown ? acc[s][i] * ldexpf(1.0f, -kDown) : acc[s][i];
                     x[s][i] = __builtin_fmaf(step, qc, z * q_sum);
                 }
+            bool lone = false;       // one token is all that this wave has
             if (!whole) {
                 // tokens that are not seen: no weight, no value, whatever
                 // their rows (nobody may have written them) and the query hold
+                int seen_here = 0;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const uint32_t begin = now.token + 16 * s;
+                    seen_here += max((int)(min(now.end[s], begin + 16) -
+                                           max(first, begin)), 0);
+                }
+                lone = seen_here == 1 && c0 + 1 == c1;
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -699,7 +709,9 @@ void attend_kernel(const Attend a) {
                 // without this one beside them)
                 const float all = over_groups(big, larger);
                 const float m_new =
-                    all > m + (kBelow + 8.0f) ? fmaxf(m, ceilf(all) - kBelow) : m;
+                    lone ? fmaxf(m, all)
+                    : all > m + (kBelow + 8.0f) ? fmaxf(m, ceilf(all) - kBelow)
+                                                : m;
                 // (from kNone: more than any exponent)
                 const int up = (int)fminf(m_new - m, 2000.0f);
                 // what p falls by the weights keep, as far as k goes
@@ -718,8 +730,9 @@ void attend_kernel(const Attend a) {
                 p[i] = __builtin_amdgcn_exp2f(
                     __builtin_fmaf(x[i >> 2][i & 3], q_scale, -m));
             // where binary32's steps are not far below 1, the logits as they are
-            // rounded, as the maximum is
-            const bool far = !(fabsf(m) < 0x1p20f);
+            // rounded, as the maximum is; so is the only one (p = 1: its value
+            // comes out as a read gives it)
+            const bool far = lone || !(fabsf(m) < 0x1p20f);
             if (__any(far)) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -876,9 +889,9 @@ void attend_kernel(const Attend a) {
             float l = 0.0f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const int by = (int)fmaxf(sm_m[w][h] - top, -2000.0f);
-                const float f = ldexpf(1.0f, by - sm_k[w][h] - down);
-                l = __builtin_fmaf(ldexpf(1.0f, by), sm_l[w][h], l);
+                const float by = __builtin_amdgcn_exp2f(sm_m[w][h] - top);
+                const float f = ldexpf(by, -sm_k[w][h] - down);
+                l = __builtin_fmaf(by, sm_l[w][h], l);
                 const f32x4 y =
                     *reinterpret_cast<const f32x4*>(&sm_o[w][h][d]);
 #pragma unroll

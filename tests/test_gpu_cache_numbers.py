@@ -326,3 +326,22 @@ def test_small_weights_beside_a_head_that_is_no_number():
     rest = np.arange(12) != 5
     assert np.array_equal(got[:, rest], out[:, rest])
     assert np.array_equal(got_lse[:, rest], lse[:, rest])
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("kbits,vbits", [(8, 4), (4, 8)])
+@pytest.mark.parametrize("window", [0, 1])
+def test_one_visible_token_is_its_value(kind, kbits, vbits, window):
+    """Bit for bit what a read gives: values of 4 bits and a step of 8 lie on
+    ties of the output's type, where any rounding of the weight shows."""
+    say(kind, kbits, vbits, window)
+    rng = np.random.default_rng(16)
+    dim, batch = 128, 48
+    f = Filled(rng, batch, 2, 16, dim, kbits, vbits)
+    n = np.ones(batch) if not window else np.r_[rng.integers(1, 17, batch - 1),
+                                                16]
+    q = queries(rng, batch, 6, dim, kind) * 3
+    out, _ = kc.attend(q, f.cache, on(np.arange(batch)[:, None]), on(n),
+                       window=window)
+    _, v = kc.read(on(np.arange(batch) * 16 + n - 1), f.cache, dim, DTYPE[kind])
+    assert torch.equal(out, v.repeat_interleave(3, 1))
