@@ -9,7 +9,7 @@
 //           the A operand (row = token, k = channel) and the queries as B
 //           (column = head), 16 tokens at a time.  Lane l gets the logits of
 //           head l % 16 for the tokens 4 (l / 16) .. + 3 of each 16.
-//   softmax the running maximum and sum of a head live in its 4 lanes.
+//   softmax the references and sums of a head live in its 4 lanes.
 //   values  O[channel][head] += V^T w, the same instruction: A = codes (row =
 //           channel, k = token), B = weights (column = head, k = token).  The
 //           order of k is free as long as A and B agree, so the weights stay
@@ -24,8 +24,9 @@
 // subnormal are bits that it loses of the sum; so 4-bit codes are taken as 16 c
 // and 8-bit keys as 4 c, a shift more for two of them (4-bit keys as c: lse off
 // by 2 to 4 10^-6, 8-bit ones as c: up to 9 10^-7, now 5 10^-7 and less; 8-bit
-// calls of one unit take 1 % longer for it, long ones as long).  float32 calls
-// centre the codes: 0x6400 | c is 1024 + c, and one packed subtraction of 1024 +
+// calls of one unit take 1 % longer for it, long ones as long).  8-bit values of
+// 16-bit calls stay c: the sums lose up to 2^-22 of their terms, against the
+// 2^-12 and 2^-9 that the outputs are rounded to.  float32 calls centre the codes: 0x6400 | c is 1024 + c, and one packed subtraction of 1024 +
 // centre (128; 8 of the 4-bit ones) gives c' = c - centre exactly, so that sums
 // do not grow by the offset and cancel again.  With z' = z + centre s (centre 0
 // where the codes are not centred) a value is s c' + z', and
@@ -36,9 +37,10 @@
 // and rounded to float16: bfloat16 and float16 values keep all their bits, but
 // for what lies below 2^-30 of the row's largest; float32 queries take a second
 // float16 for the rest (22 bits together), a second MFMA into the same
-// accumulator.  w is two float16 as well, 22 bits.  (One was 2^-12 of w c, whose magnitudes are 3
-// times the spread of the values where codes are not centred: bfloat16 outputs
-// came out a step off.)
+// accumulator.  w is two float16 as well, 22 bits.  (One, for bfloat16 calls, was
+// 2^-12 of w c, whose terms are 3 times the spread of the values where codes are
+// not centred, and moved outputs by a step; the second takes 1 % more: 128
+// sequences of 12-16 Ki tokens 516 and 521 us.)
 // Weights and the softmax's sum have references of their own.  p = 2^(logit - m),
 // m 24 below the running maximum in whole numbers, so that what float32 drops is
 // 2^-150 of the largest and less (a wave's only token has p = 1, and its value

@@ -5,7 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "bs_internal.h"   // FastDiv, quant_insert
+#include "bs_internal.h"   // FastDiv
 
 namespace bscache {
 
