@@ -296,9 +296,14 @@ __device__ __forceinline__ f32x4 mean(f32x4 r, float l) {
 __device__ __forceinline__ void finish(const Attend& a, int dtype, int64_t row,
                                        int d, float m, float l, f32x4 r) {
     store_out(a.out, row * a.c.dim + d, dtype, r);
-    if (d == 0 && a.lse)
-        a.lse[row] = l == 0.0f ? -INFINITY
-                               : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    if (d == 0 && a.lse) {
+        // l = 2^e f: m + e is exact, and small where m and e cancel
+        const int e = __builtin_amdgcn_frexp_expf(l);
+        const float f = __builtin_amdgcn_frexp_mantf(l);
+        a.lse[row] =
+            l == 0.0f ? -INFINITY
+                      : ((m + (float)e) + __builtin_amdgcn_logf(f)) * kLn2;
+    }
 }
 
 // ---- the kernel ------------------------------------------------------------

@@ -345,3 +345,19 @@ def test_one_visible_token_is_its_value(kind, kbits, vbits, window):
                        window=window)
     _, v = kc.read(on(np.arange(batch) * 16 + n - 1), f.cache, dim, DTYPE[kind])
     assert torch.equal(out, v.repeat_interleave(3, 1))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_lse_of_equal_logits_is_the_logarithm_of_their_number(kind):
+    """Sums of equal weights are exact; the logarithm of the fraction, the sum
+    with the exponent and the product with ln 2 (and ln 2 itself) are a rounding
+    each."""
+    rng = np.random.default_rng(17)
+    n = np.r_[1:40, rng.integers(40, 3000, 60)]
+    f = Filled(rng, 188, 1, 16, 64, 8, 8)
+    table = np.broadcast_to(np.arange(188), (len(n), 188)).copy()
+    q = torch.zeros((len(n), 2, 64), dtype=DTYPE[kind], device="cuda")
+    _, lse = kc.attend(q, f.cache, on(table), on(n))
+    want = np.log(n)[:, None]
+    off = np.abs(host(lse).astype(np.float64) - want)
+    assert (off <= 4 * 2.0 ** -24 * np.maximum(want, 0.5)).all(), off.max()
