@@ -42,11 +42,13 @@
 // not centred, and moved outputs by a step; the second takes 1 % more: 128
 // sequences of 12-16 Ki tokens 516 and 521 us.)
 // Weights and the softmax's sum have references of their own.  p = 2^(logit - m),
-// m 24 below the running maximum in whole numbers, so that what float32 drops is
-// 2^-150 of the largest and less (a wave's only token has p = 1, and its value
-// comes out as it is).  w = 2^k p s, with k such that the largest
-// p max(s, 2^-10 |z|) so far makes 2^6 to 2^7: a row counts by what is attended
-// to of it, and one that is not, however wide, takes no bits from the others.
+// m the running maximum up to a whole number (a wave's only token has p = 1, and
+// its value comes out as it is): the exponents of what counts are next to 0, where
+// their own rounding is least, and what float32 drops is 2^-126 of the largest
+// and less.  (24 below the maximum it was 2^-150, but float32 outputs half as far
+// off again.)  w = 2^k p s, with k such that the largest p max(s, 2^-10 |z|) so
+// far makes 2^6 to 2^7: a row counts by what is attended to of it, and one that
+// is not, however wide, takes no bits from the others.
 // (2^-10 |z|: z far beyond s is a row of nearly equal values, whose sums 2^k p z
 // would leave float32.  It is looked at only where a sum gets large.)  Both lag
 // by up to 2^8, so w stays below 2^15; it keeps its 22 bits down to 2^-9 of the
@@ -74,12 +76,8 @@
 namespace bscache {
 
 constexpr float kNone = -3.0e38f;       // reference of no logits
-// The reference m is so far below the running maximum.
-constexpr float kBelow = 24.0f;
-// k of the first tokens: the largest p is 2^(kBelow - 1) and more (where binary32
-// has no whole numbers, 1 and more), a step at least 2^-60.
+// k of the first tokens: the largest p is above 1/2, a step at least 2^-60.
 constexpr int kMost = 68;
-constexpr int kSmall = -64;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -181,8 +179,7 @@ __device__ __forceinline__ int32_t range_start(int32_t i, int32_t u, int32_t n) 
 }
 // Partial results: slot 2 i of workgroup i for the pair that began before its
 // range, 2 i + 1 for the pair that goes on behind it.  A slot holds [16][dim]
-// means and [16][2] reference and sum of p, 2^kSmall of it (the join's sums of
-// products with values near the largest stay within float32).
+// means and [16][2] reference and sum of p.
 // Behind the slots, for every pair: the workgroups of its first and last units.
 __host__ __device__ __forceinline__ int64_t part_bytes(int32_t dim) {
     return 64 * (dim + 2);
@@ -711,14 +708,13 @@ void attend_kernel(const Attend a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) big = fmaxf(big, x[s][i]);
             big *= q_scale;
-            if (__any(big > m + (kBelow + 8.0f))) {
+            if (__any(big > m + 8.0f)) {
                 // (of the heads that need it: the others stay as they would
                 // without this one beside them)
                 const float all = over_groups(big, larger);
-                const float m_new =
-                    lone ? fmaxf(m, all)
-                    : all > m + (kBelow + 8.0f) ? fmaxf(m, ceilf(all) - kBelow)
-                                                : m;
+                const float m_new = lone           ? fmaxf(m, all)
+                                    : all > m + 8.0f ? ceilf(all)
+                                                     : m;
                 // (from kNone: more than any exponent)
                 const int up = (int)fminf(m_new - m, 2000.0f);
                 // what p falls by the weights keep, as far as k goes
@@ -913,7 +909,7 @@ void attend_kernel(const Attend a) {
                 *reinterpret_cast<f32x4*>(part + h * dim + d) = r;
                 if (d == 0)
                     *reinterpret_cast<float2*>(part + 16 * dim + 2 * h) =
-                        make_float2(top, ldexpf(l, kSmall));
+                        make_float2(top, l);
             }
         }
         if (last) break;

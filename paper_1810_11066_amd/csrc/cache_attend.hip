@@ -58,21 +58,27 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a) {
                 y[u] = *reinterpret_cast<const f32x4*>(q + (h0 + h) * dim + d);
                 if (p + u * rows >= parts) ml[u].x = -INFINITY;  // not again
             }
+            // (means of means: a sum of products with values at either end
+            // would leave binary32)
             float top = m;
 #pragma unroll
             for (int u = 0; u < kDeep; ++u) top = fmaxf(top, ml[u].x);
-            const float f = __builtin_amdgcn_exp2f(m - top);
+            const float own = l * __builtin_amdgcn_exp2f(m - top);
             m = top;
-            l *= f;
-            r *= f;
+            l = own;
+            float g[kDeep];
 #pragma unroll
             for (int u = 0; u < kDeep; ++u) {
-                const float g = __builtin_amdgcn_exp2f(ml[u].x - top) * ml[u].y;
-                l += g;
+                g[u] = __builtin_amdgcn_exp2f(ml[u].x - top) * ml[u].y;
+                l += g[u];
+            }
+            const float per = l == 0.0f ? 0.0f : 1.0f / l;
+            r *= own * per;
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    r[e] = __builtin_fmaf(g, y[u][e], r[e]);
-            }
+                    r[e] = __builtin_fmaf(g[u] * per, y[u][e], r[e]);
         }
         if (rows > 1) {              // (then there is one pass over columns)
             sm_r[threadIdx.x] = r;
@@ -82,17 +88,22 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Attend a) {
                 for (int32_t w = 1; w < rows; ++w)
                     m = fmaxf(m, sm_ml[w * columns + column].x);
                 l = 0.0f;
+                for (int32_t w = 0; w < rows; ++w) {
+                    const float2 ml = sm_ml[w * columns + column];
+                    l = __builtin_fmaf(__builtin_amdgcn_exp2f(ml.x - m), ml.y,
+                                       l);
+                }
+                const float per = l == 0.0f ? 0.0f : 1.0f / l;
                 r = f32x4{0, 0, 0, 0};
                 for (int32_t w = 0; w < rows; ++w) {
                     const float2 ml = sm_ml[w * columns + column];
-                    const float f = __builtin_amdgcn_exp2f(ml.x - m);
-                    l = __builtin_fmaf(f, ml.y, l);
-                    r += f * sm_r[w * columns + column];
+                    r += __builtin_amdgcn_exp2f(ml.x - m) * ml.y * per *
+                         sm_r[w * columns + column];
                 }
             }
         }
         if (on && mine == 0)
-            finish(a, a.dtype, row0 + h, d, m, ldexpf(l, -kSmall), mean(r, l));
+            finish(a, a.dtype, row0 + h, d, m, l, r);
     }
 }
 
