@@ -137,8 +137,9 @@ bscache_status bscache_read(const bscache_pages *cache, const int32_t *slots,
  * Products are of the exact codes: q enters the matrix units scaled by a power
  * of two as float16 (bfloat16 and float16 values keep their bits but for what
  * lies below 2^-30 of the row's largest; float32 as two float16 of 22 bits
- * together), weights times s as two float16 of 22 bits together; sums and the
- * softmax are binary32.
+ * together), weights times s as two float16 of 22 bits together, and to 2^-31 of
+ * the largest weight times max(s, 2^-10 |z|); sums and the softmax are binary32,
+ * weights below 2^-126 of the largest 0.
  * The workspace holds partial results of sequences that several workgroups
  * share: bscache_attend_workspace() bytes (0 for short max_len), 16-byte
  * aligned, contents irrelevant before and after.

@@ -1,9 +1,10 @@
 // Attention of one new token over the pages of a quantized cache.
 //
 // A workgroup takes units of 128 tokens of one (sequence, key-value head, tile
-// of up to 16 query heads); its four waves take 32 tokens of a unit each and
-// never wait for one another until the pair ends.  (The wide form is as many
-// waves as a CU holds, and units of 32 tokens for each.)  Per wave and unit:
+// of up to 16 query heads; more heads are more tiles, each of which reads the rows
+// by itself); its four waves take 32 tokens of a unit each and never wait for one
+// another until the pair ends.  (The wide form is as many waves as a CU holds, and
+// units of 32 tokens for each.)  Per wave and unit:
 //
 //   logits  S[token][head] = K q as v_mfma_f32_16x16x32_f16 with the codes as
 //           the A operand (row = token, k = channel) and the queries as B
@@ -120,9 +121,9 @@ __device__ __forceinline__ int32_t wave_scan(int32_t v) {
 }
 
 // Places of a pair in the row: its units, then an empty one for what it costs to
-// begin and end a pair (4.6 us, against 1.3 us a unit where a workgroup has one
+// begin and end a pair (5 us, against 1.2 us a unit where a workgroup has one
 // or two pairs, and 2.6 us where it has many and the memory is busy; at least 3
-// places a pair: 1000 sequences of 1-4096 tokens 284 us for 272).
+// places a pair: 1000 sequences of 1-4096 tokens 263 us for 253).
 __device__ __forceinline__ int32_t pair_places(int32_t units) {
     return units + 1;
 }
@@ -332,7 +333,7 @@ __device__ __forceinline__ Rsrc rows_buffer(const void* base, int64_t at,
 // the non-temporal policy: one instruction takes whole lines of them, and they
 // leave the caches to the rest (100 sequences of 500-3000 tokens 85 -> 79 us).
 // Keys and 4-bit values come by two instructions a line, and the second one
-// would often find it gone (128 x 12-16 Ki tokens, 4-bit values 518 -> 538 us).
+// would often find it gone (128 x 12-16 Ki tokens, 4-bit values 521 -> 551 us).
 constexpr int kOnce = 2;
 template <int POLICY, int N>
 __device__ __forceinline__ void load_words(Rsrc rows, uint32_t at,

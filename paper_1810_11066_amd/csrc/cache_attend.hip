@@ -117,31 +117,32 @@ template <> hipError_t launch_attend_dp<256>(const Attend&, hipStream_t);
 // head tiles, and the tokens that the longest sequence may span.
 //
 // A pair to one workgroup needs no plan of the lengths and no join (4 us and a
-// launch), but the longest pair sets the time: 4 us and 1.3 us a unit of
-// 128 tokens.  Up to 4 units that is always shorter (8 pairs of 4 units 8.8 us whole
-// and 9.8 shared, of 8 units 14.5 and 9.9; 128 pairs of 4 units 10.1 and 12.6).
+// launch), but the longest pair sets the time: 5 us and 1.2 us a unit of
+// 128 tokens.  Up to 4 units that is always shorter (8 pairs of 4 units 9.7 us whole
+// and 10.5 shared, of 8 units 14.5 and 10.6; 128 pairs of 4 units 11.1 and 13.5).
 // Longer ones win where the pairs fill the GPU anyway: up to 8 units with a pair
-// for every CU (320 pairs of 8 units 22.0 and 24.9 us), up to 16 with pairs for
-// half of the workgroups that run at once (512 pairs of 16 units 56 and 60 us, 64
-// channels 31.7 and 33.3).  Lengths from a quarter of the longest to all of it
-// leave that so (384 pairs of 375 to 1500 tokens 27.5 and 27.2, 2000 pairs 112 and
-// 119); where few are long, what the longest takes is lost (lengths spread by
-// their logarithm from 1: to 1000 tokens 16.5 and 16.8, to 2000 27.8 and 18.5).
+// for every CU (320 pairs of 8 units 23.7 and 26.6 us), up to 16 with pairs for
+// half of the workgroups that run at once (512 pairs of 16 units 57.6 and 63.7 us,
+// 64 channels 35.8 and 36.0).  Lengths from a quarter of the longest to all of it
+// leave that so (384 pairs of 375 to 1500 tokens 29.4 and 28.1, 2000 pairs 99 and
+// 108); where few are long, what the longest takes is lost (384 pairs of lengths
+// spread by their logarithm from 1: to 1000 tokens 17.5 and 17.5, to 2000 29.1 and
+// 19.3).
 //
 // With fewer pairs than CUs a workgroup can have its CU to itself: the wide
 // form, of as many waves as the CU holds (8 to 16).  A CU's own rate of reading
 // bounds it, so it needs pairs on a quarter of the CUs, and sequences of more
-// than 4 units that it takes in 4 steps (128 pairs of 748 tokens 11.7 us wide,
-// 14.4 shared; of 1132 13.9 and 16.9; of 1516 16.6 and 18.2; 64 pairs 11.1 and
-// 12.0, 13.5 and 14.0, 16.1 and 14.6).
+// than 4 units that it takes in 4 steps (128 pairs of 748 tokens 12.3 us wide,
+// 15.2 shared; of 1132 14.8 and 17.7; of 1516 17.2 and 18.9; 64 pairs 11.7 and
+// 12.6, 14.3 and 14.6, 16.9 and 15.3).
 //
 // Everything else is shared: as many workgroups as run at once, each with its
 // part (4 times as many, taken up as others end: 551 us for 524 at 128
 // sequences of 12-16 Ki tokens).  The join takes all heads of a tile together
-// where pairs are many (64 ragged sequences 28.6 us, 30.5 head by head), and
+// where pairs are many (64 ragged sequences 32.2 us, 34.3 head by head), and
 // where one round of loads does for as many partial results as a sequence may
-// have (16 x 2048 tokens 20.2 and 20.8); otherwise it takes them one by one (1 x
-// 8192 tokens 12.8 us, 14.6 together; 256 channels 29.2 and 36.1).
+// have (16 x 2048 tokens 21.8 and 22.7); otherwise it takes them one by one (1 x
+// 8192 tokens 13.7 us, 15.7 together; of 256 channels 18.0 and 21.5).
 void plan_attend(Attend& a, int64_t tokens) {
     const int64_t pairs = (int64_t)a.batch * a.c.kv_heads * a.head_tiles;
     const int dp = padded_dim(a.c.dim);
